@@ -28,6 +28,9 @@ __all__ = [
     "topk_select", "sparse_attn", "full_attn", "gemm_rows", "gemm_rows_split", "rmsnorm_rows", "rope_rows",
     "silu_mul_rows", "F32", "BF16", "ROPE_NEOX", "ROPE_GPTJ", "TOPK_ALL_POSITIONS", "EXPORTED", "use_checked",
     "RELEASE_LIB_PATH", "CHECKED_LIB_PATH",
+    # decoding over a 4-bit cache (decode.py)
+    "append_slots", "qk_norm_rope", "qk_norm_rope_rows", "kv4_record_bytes", "kv4_write", "kv4_read", "kv4_pack",
+    "kv4_unpack", "kv4_attn_workspace", "kv4_attn",
 ]
 
 RELEASE_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsx.so")
@@ -45,6 +48,9 @@ EXPORTED = (
     "sx_realign_scatter_masked", "sx_sparseq_score", "sx_sparseq_score_static", "sx_topk_select",
     "sx_sparse_attn", "sx_full_attn", "sx_gemm_rows", "sx_gemm_rows_split", "sx_rmsnorm_rows", "sx_rope_rows", "sx_silu_mul_rows",
     "sx_last_error", "sx_version",
+    # include/sx_decode.h
+    "sx_append_slots", "sx_qk_norm_rope", "sx_qk_norm_rope_rows", "sx_kv4_record_bytes", "sx_kv4_write", "sx_kv4_read",
+    "sx_kv4_pack", "sx_kv4_unpack", "sx_kv4_attn_workspace", "sx_kv4_attn",
 )
 
 
@@ -120,6 +126,16 @@ def lib() -> ctypes.CDLL:
         L.sx_rmsnorm_rows.argtypes = [VP, VP, VP, I32, VP, I32, VP, F, I32, VP, I32, VP]
         L.sx_rope_rows.argtypes = [VP, VP, VP, I32, VP, VP, VP]
         L.sx_silu_mul_rows.argtypes = [VP, VP, I32, VP, I32, VP, VP]
+        L.sx_append_slots.argtypes = [VP, VP, I32, I32, VP, I32, VP, VP, I32, I32, VP, VP, VP, VP, VP, VP]
+        L.sx_qk_norm_rope.argtypes = [VP, VP, I64, VP, I64, VP, VP, F, VP, I32, VP, I64, VP, I64, VP]
+        L.sx_qk_norm_rope_rows.argtypes = [VP, VP, VP, I32, VP, VP, VP, VP, F, VP]
+        L.sx_kv4_record_bytes.argtypes = [VP, P(I64)]
+        L.sx_kv4_write.argtypes = [VP, VP, I64, VP, I64, VP, I32, VP, I64, VP]
+        L.sx_kv4_read.argtypes = [VP, VP, I64, VP, I32, VP, I64, VP, I64, VP]
+        L.sx_kv4_pack.argtypes = [VP, VP, VP, I64, VP, I32, VP, I64, VP, VP]
+        L.sx_kv4_unpack.argtypes = [VP, VP, I64, VP, I32, VP, VP, I64, VP, VP]
+        L.sx_kv4_attn_workspace.argtypes = [VP, I32, I32, I32, P(I64)]
+        L.sx_kv4_attn.argtypes = [VP, VP, I64, VP, VP, VP, I32, I32, I32, I32, I32, VP, I64, VP, VP, VP, I64, VP]
         for name in EXPORTED:
             if name in ("sx_last_error", "sx_version"):
                 getattr(L, name).restype = ctypes.c_char_p
@@ -341,3 +357,15 @@ def silu_mul_rows(plan: Plan, n_rows, max_rows: int, gate_up, y, stream=None):
     f = int(y.shape[-1])
     _check(lib().sx_silu_mul_rows(plan.handle, _ptr(n_rows), int(max_rows), _ptr(gate_up), f, _ptr(y),
                                   _stream(stream)))
+
+
+# ---- decoding over a 4-bit cache (see include/sx_decode.h) ----
+
+def __getattr__(name):
+    """The calls of decode.py, loaded with torch on their first use."""
+    if name in ("append_slots", "qk_norm_rope", "qk_norm_rope_rows", "kv4_record_bytes", "kv4_write", "kv4_read", "kv4_pack",
+                "kv4_unpack", "kv4_attn_workspace", "kv4_attn"):
+        from . import decode
+        globals()[name] = getattr(decode, name)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

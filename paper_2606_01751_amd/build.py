@@ -51,12 +51,13 @@ def _compile(src: str, debug: bool, checked: bool = False) -> str:
 def build(debug: bool = False, jobs: int = 8) -> str:
     os.makedirs(BUILD, exist_ok=True)
     sources = sorted(glob.glob(os.path.join(CSRC, "*.hip"))) + sorted(glob.glob(os.path.join(CSRC, "*.cpp")))
-    host = os.path.join(CSRC, "sx_host.cpp")   # the only source the device checks change
+    hosts = [os.path.join(CSRC, f) for f in ("sx_host.cpp", "sx_decode.cpp")]   # the sources the device checks change
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(lambda s: _compile(s, debug), sources))
-        host_checked = ex.submit(_compile, host, debug, True).result()
+        checked = list(ex.map(lambda s: _compile(s, debug, True), hosts))
     _link(objs, LIB)
-    _link([host_checked if o.endswith("sx_host.cpp.o") else o for o in objs], LIB_CHECKED)
+    plain = [os.path.join(BUILD, os.path.basename(h) + ".o") for h in hosts]
+    _link([checked[plain.index(o)] if o in plain else o for o in objs], LIB_CHECKED)
     return LIB
 
 

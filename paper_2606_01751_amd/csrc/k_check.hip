@@ -9,8 +9,10 @@
 // Row lists (row-list layout of include/sx.h), per request r with n = n_rows[r]:
 //   0 <= n <= T_r; the first min(n, max_rows) rows are in [0, T_r) and strictly ascending.
 // cu_seqlens: cu[0] = 0 and 0 <= cu[r + 1] - cu[r] <= max_seqlen.
+// The decoding calls (include/sx_decode.h): lengths >= 0, indices (slots, block ids) from -1 up to their
+// bound, and for the attention cu_q as cu_seqlens, within total_q, and the block table entries of every key.
 // The checks read only in-bounds entries: at most T_r rows of a request's own region.
-#include "sx_internal.h"
+#include "sx_kv4.h"
 
 namespace sx {
 namespace {
@@ -18,7 +20,8 @@ namespace {
 // verdict of the last check: code (0 = valid), request, index, value
 __device__ int g_check[4];
 
-enum { kBadCount = 1, kRowRange = 2, kRowOrder = 3, kCuStart = 4, kCuLength = 5 };
+enum { kBadCount = 1, kRowRange = 2, kRowOrder = 3, kCuStart = 4, kCuLength = 5, kBadLength = 6, kBadIndex = 7, kBadTable = 8,
+       kCuEnd = 9 };
 
 __device__ void report_bad(int code, int r, int i, int v) {
   if (atomicCAS(&g_check[0], 0, code) == 0) {
@@ -55,6 +58,36 @@ __global__ __launch_bounds__(256) void check_cu_kernel(const int32_t* __restrict
   if (len < 0 || len > max_seqlen) report_bad(kCuLength, r, r, len);
 }
 
+__global__ __launch_bounds__(256) void check_lengths_kernel(const int32_t* __restrict__ ctx, const int32_t* __restrict__ add,
+                                                            int n_req) {
+  const int r = blockIdx.x * blockDim.x + threadIdx.x;
+  if (r >= n_req) return;
+  const int c = ctx[r], n = add ? add[r] : 1;
+  if (c < 0) report_bad(kBadLength, r, r, c);
+  else if (n < 0 || n > INT32_MAX - c) report_bad(kBadLength, r, r, n);
+}
+
+__global__ __launch_bounds__(256) void check_index_kernel(const int32_t* __restrict__ idx, int n, int64_t limit) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n && (idx[i] < -1 || idx[i] >= limit)) report_bad(kBadIndex, 0, i, idx[i]);
+}
+
+__global__ __launch_bounds__(256) void check_kv4_kernel(Kv4AttnK a) {   // one workgroup per request
+  const int r = blockIdx.x;
+  const int n = a.cu[r + 1] - a.cu[r], len = a.lens[r];
+  if (threadIdx.x == 0) {
+    if (r == 0 && a.cu[0] != 0) report_bad(kCuStart, 0, 0, a.cu[0]);
+    if (n < 0 || n > a.max_q) report_bad(kCuLength, r, r, n);
+    if (r == a.n_req - 1 && a.cu[r + 1] > a.total_q) report_bad(kCuEnd, r, r + 1, a.cu[r + 1]);
+    if (len < 0 || len > a.max_seqlen || len > (int64_t)a.max_blocks * kBlock) report_bad(kBadLength, r, r, len);
+  }
+  const int64_t blocks = min(((int64_t)max(len, 0) + kBlock - 1) / kBlock, (int64_t)a.max_blocks);
+  for (int64_t i = threadIdx.x; i < blocks; i += 256) {
+    const int id = a.table[(int64_t)r * a.max_blocks + i];
+    if (id < -1 || id >= a.n_blocks) report_bad(kBadTable, r, (int)i, id);
+  }
+}
+
 // Launch status, then the verdict (synchronises the stream).  *code = 0 when valid.
 hipError_t read_verdict(hipStream_t s, int out[4]) {
   hipError_t e = hipGetLastError();
@@ -78,6 +111,24 @@ hipError_t device_check_rows(const sx_plan* p, const int32_t* rows, const int32_
 hipError_t device_check_cu(const int32_t* cu, int32_t n_req, int32_t max_seqlen, hipStream_t s, int verdict[4]) {
   hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
   hipLaunchKernelGGL(check_cu_kernel, dim3((unsigned)((n_req + 255) / 256)), dim3(256), 0, s, cu, n_req, max_seqlen);
+  return read_verdict(s, verdict);
+}
+
+hipError_t device_check_lengths(const int32_t* ctx, const int32_t* add, int32_t n_req, hipStream_t s, int verdict[4]) {
+  hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
+  hipLaunchKernelGGL(check_lengths_kernel, dim3((unsigned)((n_req + 255) / 256)), dim3(256), 0, s, ctx, add, n_req);
+  return read_verdict(s, verdict);
+}
+
+hipError_t device_check_index(const int32_t* idx, int32_t n, int64_t limit, hipStream_t s, int verdict[4]) {
+  hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
+  hipLaunchKernelGGL(check_index_kernel, dim3((unsigned)(((int64_t)n + 255) / 256)), dim3(256), 0, s, idx, n, limit);
+  return read_verdict(s, verdict);
+}
+
+hipError_t device_check_kv4(const Kv4AttnK& a, hipStream_t s, int verdict[4]) {
+  hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
+  hipLaunchKernelGGL(check_kv4_kernel, dim3((unsigned)a.n_req), dim3(256), 0, s, a);
   return read_verdict(s, verdict);
 }
 

@@ -66,6 +66,15 @@ sx_status report(sx_status st, const char* msg) {
   g_err = msg;
   return st;
 }
+sx_status reportf(sx_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return st;
+}
 }  // namespace sx
 
 namespace {
@@ -108,6 +117,20 @@ constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - ((int64_t)1 << 16);
 float effective_scale(const sx_layer_desc* d) {
   return d->softmax_scale > 0.0f ? d->softmax_scale : (float)(1.0 / std::sqrt((double)d->head_dim));
 }
+
+}  // namespace
+
+namespace sx {
+sx_status check_desc(const sx_layer_desc* d) { return validate_desc(d); }
+sx_status launch_status(hipError_t e, const char* what) { return check_launch(e, what); }
+float softmax_scale(const sx_layer_desc* d) { return effective_scale(d); }
+sx_status check_row_list(const sx_plan* p, const int32_t* rows, const int32_t* n_rows, int32_t max_rows, void* stream,
+                         const char* who) {
+  return device_rows_ok(p, rows, n_rows, max_rows, stream, who);
+}
+}  // namespace sx
+
+namespace {
 
 template <typename T>
 sx_status dev_alloc(sx_plan* p, T** ptr, size_t count) {

@@ -160,6 +160,14 @@ hipError_t device_check_cu(const int32_t* cu, int32_t n_req, int32_t max_seqlen,
 // Sets the thread-local error message read by sx_last_error and returns st (for host-only
 // translation units without the dispatcher's helpers).
 sx_status report(sx_status st, const char* msg);
+sx_status reportf(sx_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// The dispatcher's checks for the other host translation units: descriptor, launch status, softmax scale
+// actually used, and (checked library) a plan's row list.
+sx_status check_desc(const sx_layer_desc* d);
+sx_status launch_status(hipError_t e, const char* what);
+float softmax_scale(const sx_layer_desc* d);
+sx_status check_row_list(const sx_plan* p, const int32_t* rows, const int32_t* n_rows, int32_t max_rows, void* stream,
+                         const char* who);
 
 struct RowsArg {
   const int32_t* rows;

@@ -1,0 +1,124 @@
+// Internal declarations of the decoding calls (include/sx_decode.h), shared by their host side and kernels.
+#pragma once
+
+#include "sx_decode.h"
+#include "sx_internal.h"
+
+namespace sx {
+
+// ---- the 4-bit record of one KV head of one block (include/sx_decode.h) ----
+constexpr int kKv4Group = 32;   // elements that share a scale
+__host__ __device__ constexpr int kv4_record(int d) { return 17 * d; }
+__host__ __device__ constexpr int kv4_v_codes(int d) { return 8 * d; }
+__host__ __device__ constexpr int kv4_k_scales(int d) { return 16 * d; }
+__host__ __device__ constexpr int kv4_v_scales(int d) { return 16 * d + d / 2; }
+
+// ---- split of a request's keys over workgroups ----
+// A request of `rows` query rows per KV head (tokens x group) and `len` keys is cut into chunks of equal
+// length, by its own sizes alone, so that its result does not depend on the rest of the batch: at least
+// kKv4Chunk keys each, at most kKv4Splits of them, and at most kKv4PartRows partial rows in all (few rows
+// need the split to fill the chip; many rows fill it by themselves).
+constexpr int kKv4Chunk = 512;
+constexpr int kKv4Splits = 64;
+constexpr int kKv4PartRows = 4096;
+constexpr int kKv4Step = 128;    // a chunk's length is a multiple of this
+struct Kv4Split {
+  int n, keys;   // chunks, and keys of each but the last
+};
+__host__ __device__ inline Kv4Split kv4_split(int rows, int len) {
+  const int r16 = rows <= 16 ? 16 : rows;
+  int cap = kKv4PartRows / r16;
+  cap = cap < 1 ? 1 : cap > kKv4Splits ? kKv4Splits : cap;
+  int n = (int)(((int64_t)len + kKv4Chunk - 1) / kKv4Chunk);
+  n = n < 1 ? 1 : n > cap ? cap : n;
+  const int64_t per = ((int64_t)len + n - 1) / n;
+  const int64_t keys = (per + kKv4Step - 1) / kKv4Step * kKv4Step;
+  const int64_t used = keys > 0 ? ((int64_t)len + keys - 1) / keys : 1;
+  return {(int)(used < 1 ? 1 : used), (int)(keys > INT32_MAX ? INT32_MAX : keys)};
+}
+// most chunks, and most partial rows (rows x chunks, where there is more than one chunk), of a request of
+// at most `rows` rows and `len` keys
+inline int kv4_max_chunks(int len) {
+  const int64_t n = ((int64_t)len + kKv4Chunk - 1) / kKv4Chunk;
+  return (int)(n < 1 ? 1 : n > kKv4Splits ? kKv4Splits : n);
+}
+inline int64_t kv4_part_rows(int64_t rows, int len) {
+  const int c = kv4_max_chunks(len);
+  if (c <= 1) return 0;
+  const int64_t n = (rows < kKv4PartRows ? rows : kKv4PartRows) * c;
+  return n < kKv4PartRows ? n : kKv4PartRows;
+}
+
+struct AppendSlotsK {
+  const int32_t* ctx;
+  const int32_t* add;        // may be null: one token each
+  const int32_t* free_blocks;
+  const int32_t* free_head;  // may be null
+  int32_t* table;
+  int32_t* seq;
+  int32_t* cu;
+  int32_t* pos;
+  int32_t* slots;
+  int32_t* state;
+  int n_req, block, n_free, max_blocks, max_tokens;
+};
+hipError_t launch_append_slots(const AppendSlotsK& a, hipStream_t s);
+
+struct QkNormRopeK {
+  const void* q;
+  const void* k;
+  void* qo;
+  void* ko;
+  int64_t q_ld, k_ld, qo_ld, ko_ld;   // elements between token rows
+  const void* gq;                     // may be null
+  const void* gk;
+  float eps;
+  int n, Hq, Hkv;
+  const int32_t* pos;                 // [n] by token row
+  double theta[64];                   // frequencies (plan calls: the plan's array instead)
+  // plan's row list
+  const ReqDev* reqs;
+  const int32_t* rows;
+  const int32_t* n_rows;
+  const int32_t* tok_pos;
+  const double* d_theta;
+  int max_rows, n_req;
+};
+hipError_t launch_qk_norm_rope(const QkNormRopeK& a, int D, bool f32, bool neox, hipStream_t s);
+
+struct Kv4MoveK {
+  void* k;              // 16- or 32-bit side
+  void* v;
+  int64_t k_ld, v_ld;   // rows: elements between token rows
+  const int32_t* idx;   // slots, or pool blocks
+  const int32_t* cache_blocks;   // blocks only
+  uint8_t* pool;
+  int64_t n_blocks, n_cache_blocks;
+  int n, Hkv;
+};
+hipError_t launch_kv4_write(const Kv4MoveK& a, int D, bool f32, bool blocks, hipStream_t s);
+hipError_t launch_kv4_read(const Kv4MoveK& a, int D, bool f32, bool blocks, hipStream_t s);
+
+struct Kv4AttnK {
+  const void* q;
+  int64_t q_ld;
+  const int32_t* cu;
+  const int32_t* lens;
+  const int32_t* table;
+  const uint8_t* pool;
+  void* out;
+  float* lse;
+  float* part;          // [n_req][Hkv][part_rows][D] unnormalised partial outputs
+  float2* part_ml;      // [n_req][Hkv][part_rows] (max, sum), base-2 scores
+  int64_t n_blocks, part_rows;
+  int max_blocks, n_req, total_q, max_q, max_seqlen, Hq, Hkv;
+  float scale;          // softmax scale * log2(e)
+};
+hipError_t launch_kv4_attn(const Kv4AttnK& a, int D, bool f32, hipStream_t s);
+
+// Checked library: device-side validation (synchronises the stream); verdict as in sx_internal.h.
+hipError_t device_check_lengths(const int32_t* ctx, const int32_t* add, int32_t n_req, hipStream_t s, int verdict[4]);
+hipError_t device_check_index(const int32_t* idx, int32_t n, int64_t limit, hipStream_t s, int verdict[4]);
+hipError_t device_check_kv4(const Kv4AttnK& a, hipStream_t s, int verdict[4]);
+
+}  // namespace sx

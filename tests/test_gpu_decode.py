@@ -1,0 +1,652 @@
+"""Decoding over a 4-bit cache on the GPU against float64 references (kv4ref.py).
+
+Rounding: an output is off by at most half a step of its type, eps / 2 relative (plus the smallest normal times it);
+what the float32 arithmetic before it may add is derived in kv4ref.py."""
+import math
+
+import pytest
+import torch
+
+import kv4ref as R
+import paper_2606_01751_amd as sx
+import workloads as W
+from sxgpu import desc_of, log
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    sx.lib()
+
+
+def i32(x):
+    return torch.as_tensor(x, dtype=torch.int32).cuda()
+
+
+def near(got, want, bound, what):
+    got = got.double().cpu()
+    eps = torch.finfo(torch.bfloat16 if what.endswith("bf16") else torch.float32).eps
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN in other places"
+    off = (got - want).abs() - (bound + eps / 2 * (want.abs() + bound) + 1e-37)
+    worst = off.nan_to_num(-1.0).max().item() if off.numel() else 0.0
+    assert worst <= 0, f"{what}: over the bound by {worst}"
+
+
+# ---------------------------------------------------------------- slot maps
+
+def run_slots(ctx, new, b, free, head, table, room, none=False):
+    n = len(ctx)
+    t = table.cuda()
+    seq, cu, pos, slot, state = (torch.full((k,), -77, dtype=torch.int32, device="cuda") for k in (n, n + 1, room, room, 2))
+    sx.append_slots(i32(ctx), None if none else i32(new), i32(free), t, seq, cu, pos, slot, state,
+                    free_head=i32([head]), block_size=b)
+    return [x.cpu() for x in (t, seq, cu, pos, slot, state)]
+
+
+def check_slots(ctx, new, b, free, head, table, room, none=False):
+    got = run_slots(ctx, new, b, free, head, table, room, none)
+    want = R.append_slots(ctx, new, b, free, head, table, room)
+    for name, g, w in zip(("table", "seq", "cu", "pos", "slot", "state"), got, want):
+        assert torch.equal(g, torch.as_tensor(w, dtype=torch.int32).reshape(g.shape)), name
+
+
+@pytest.mark.parametrize("n,b,spread,room_more,width,seed", [
+    (1, 16, 1, 0, 8, 0), (1, 16, 200, 3, 8, 1), (3, 16, 40, 5, 6, 2), (64, 16, 1, 0, 40, 3), (255, 16, 60, 9, 30, 4),
+    (256, 16, 33, 0, 30, 5), (257, 1, 9, 4, 64, 6), (700, 5, 90, 1000, 90, 7), (2000, 16, 7, 2, 20, 8), (4, 16, 9000, 0, 700, 9),
+])
+def test_append_slots(n, b, spread, room_more, width, seed):
+    g = torch.Generator().manual_seed(seed)
+    ctx = [0 if c % 5 == 0 else c for c in torch.randint(0, b * width // 2 + 1, (n,), generator=g).tolist()]
+    new = torch.randint(0 if spread > 1 else 1, spread + 1, (n,), generator=g).tolist()
+    table = torch.full((n, width), -9, dtype=torch.int32)
+    nxt = 0
+    for r in range(n):
+        k = min(-(-ctx[r] // b), width)
+        table[r, :k] = torch.arange(nxt, nxt + k)
+        nxt += k
+    free = (torch.randperm(sum(new) // b + 2 * n + 5, generator=g) + nxt).tolist()
+    check_slots(ctx, new, b, free, 2, table, sum(new) + room_more)
+
+
+def test_append_slots_short_lists_and_rooms():
+    table = torch.full((4, 3), -9, dtype=torch.int32)
+    table[0, :2], table[1, 0], table[3, :3] = torch.tensor([5, -1]), 6, torch.tensor([7, 8, 9])
+    ctx, new = [20, 10, 0, 48], [30, 10, 20, 4]     # an entry of request 0 is missing, request 3's table is full
+    for free, head in (([11, 12, 13, 14, 15], 0), ([11, 12], 0), ([11, 12, 13], 2), ([], 0), ([11], 9)):
+        for room in (0, 1, 37, 64, 70):
+            check_slots(ctx, new, 16, free, head, table.clone(), room)
+
+
+def test_append_slots_one_token_each_and_negative_lengths():
+    table = torch.arange(12, dtype=torch.int32).view(3, 4)
+    check_slots([15, 16, 0], [1, 1, 1], 16, [20, 21, 22], 0, table, 5, none=True)
+    got = run_slots([-5, 3, 0], [2, -7, 0], 16, [30, 31], 0, table, 4)
+    want = R.append_slots([0, 3, 0], [2, 0, 0], 16, [30, 31], 0, table, 4)
+    for g, w in zip(got, want):
+        assert torch.equal(g, torch.as_tensor(w, dtype=torch.int32).reshape(g.shape))
+
+
+def test_append_slots_beyond_32_bits():
+    # lengths whose sums pass 2^31 saturate, and a slot that int32 cannot hold is refused
+    big = (1 << 31) - 17
+    table = torch.zeros(3, 1, dtype=torch.int32)
+    t, seq, cu, pos, slot, state = run_slots([0, 0, 5], [big, big, 1], 16, [1 << 28], 0, table, 20)
+    assert cu.tolist() == [0, big, (1 << 31) - 1, (1 << 31) - 1] and seq.tolist() == [big, big, 6]
+    assert pos.tolist() == list(range(20)) and slot.tolist() == [-1] * 20
+    assert state[1] == (1 << 31) - 1
+
+
+# ---------------------------------------------------------------- norm and rotation
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,n,neox,norm,packed", [
+    (8, 2, 128, 1, True, True, False), (32, 8, 128, 5, True, True, True), (28, 4, 128, 67, False, True, True),
+    (1, 1, 64, 3, True, True, False), (7, 7, 64, 130, False, True, True), (8, 1, 128, 33, True, False, True),
+    (64, 1, 64, 9, True, True, False), (3, 1, 128, 1000, True, True, True),
+])
+def test_qk_norm_rope(dtype, hq, hkv, d, n, neox, norm, packed):
+    g = torch.Generator().manual_seed(n + d)
+    dt = DT[dtype]
+    x = (torch.randn(n, hq + 2 * hkv, d, generator=g) * torch.exp(torch.randn(n, hq + 2 * hkv, 1, generator=g))).to(dt)
+    x[0, 0] = 0
+    gq, gk = ((1 + 0.3 * torch.randn(d, generator=g)).to(dt) for _ in range(2))
+    pos = torch.randint(0, 1 << 20, (n,), generator=g, dtype=torch.int32)
+    pos[::7] = -1 if n > 1 else 5
+    if n > 4:
+        pos[4] = (1 << 31) - 1
+    xd = x.cuda()
+    q, k = (xd[:, :hq], xd[:, hq:hq + hkv]) if packed else (xd[:, :hq].contiguous(), xd[:, hq:hq + hkv].contiguous())
+    qo, ko = (torch.full((n, h, d), -7.0, dtype=dt, device="cuda") for h in (hq, hkv))
+    desc = sx.make_desc(hq, hkv, d, dtype, 1e6, "neox" if neox else "gptj")
+    kw = dict(gamma_q=gq.cuda(), gamma_k=gk.cuda()) if norm else {}
+    sx.qk_norm_rope(desc, q, k, pos.cuda(), qo, ko, eps=1e-5, **kw)
+    live = pos >= 0
+    for got, src, gam, name in ((qo, x[:, :hq], gq, "q"), (ko, x[:, hq:hq + hkv], gk, "k")):
+        want, bound = R.norm_rope(src, gam if norm else None, 1e-5, pos.clamp(min=0), 1e6, neox)
+        assert (got.cpu()[~live] == -7).all()
+        near(got.cpu()[live], want[live], bound[live], f"{name} {dtype}")
+    # in place gives the same bits, and only one of the two scaled
+    sx.qk_norm_rope(desc, q, k, pos.cuda(), q, k, eps=1e-5, **kw)
+    assert torch.equal(q[live.cuda()], qo[live.cuda()]) and torch.equal(k[live.cuda()], ko[live.cuda()])
+    assert torch.equal(xd[:, hq + hkv:].cpu(), x[:, hq + hkv:]) or not packed
+
+
+@pytest.mark.parametrize("one", ["gamma_q", "gamma_k"])
+def test_qk_norm_rope_with_one_gamma(one):
+    d, n = 64, 6
+    x = torch.randn(n, 4, d).cuda()
+    gam = (1 + 0.1 * torch.randn(d)).cuda()
+    pos = i32(range(n))
+    qo, ko = torch.empty(n, 3, d, device="cuda"), torch.empty(n, 1, d, device="cuda")
+    sx.qk_norm_rope(sx.make_desc(3, 1, d, "f32", 1e4), x[:, :3], x[:, 3:], pos, qo, ko, eps=1e-6, **{one: gam})
+    for got, src, name in ((qo, x[:, :3], "gamma_q"), (ko, x[:, 3:], "gamma_k")):
+        want, bound = R.norm_rope(src.cpu(), gam.cpu() if name == one else None, 1e-6, pos.cpu(), 1e4, True)
+        near(got, want, bound, "f32")
+
+
+def test_qk_norm_rope_is_independent_of_the_batch():
+    d = 128
+    x = torch.randn(300, 12, d).bfloat16().cuda()
+    pos = torch.randint(0, 9999, (300,), dtype=torch.int32).cuda()
+    gam = torch.ones(d).bfloat16().cuda()
+    desc = sx.make_desc(8, 2, d, "bf16", 1e6)
+
+    def go(a, b):
+        qo, ko = (torch.empty(b - a, h, d, dtype=torch.bfloat16, device="cuda") for h in (8, 2))
+        sx.qk_norm_rope(desc, x[a:b, :8], x[a:b, 8:10], pos[a:b].clone(), qo, ko, gamma_q=gam, gamma_k=gam)
+        return qo, ko
+    full = go(0, 300)
+    for a, b in ((0, 1), (17, 18), (130, 299)):
+        part = go(a, b)
+        assert torch.equal(part[0], full[0][a:b]) and torch.equal(part[1], full[1][a:b])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_qk_norm_rope_rows(dtype, d):
+    specs = [[(37, False, 0, None), (250, True, 900, None), (5, False, 0, None)], [(20, True, 0, 50), (30, False, 0, 70)]]
+    w = W.custom_workload(specs, n_q_heads=8, n_kv_heads=2, head_dim=d, dtype=dtype, rope_base=5e5, seed=7, name="rows")
+    plan = sx.Plan(desc_of(w), w.requests, w.n_dst_blocks, w.n_src_blocks)
+    T, dt = w.total_tokens, DT[dtype]
+    lists = [list(range(0, 292, 3)), [0, 7, 19, 20, 49]]
+    rows, offs, pos = torch.zeros(T, dtype=torch.int32), w.token_offsets, torch.full((T,), -1, dtype=torch.int32)
+    for r, req in enumerate(w.requests):
+        rows[offs[r]:offs[r] + len(lists[r])] = torch.tensor(lists[r])
+        for t in lists[r]:
+            s = next(s for s in req.segments if s.seq_start <= t < s.seq_start + s.length)
+            pos[offs[r] + t] = s.new_pos + t - s.seq_start
+    q, k = torch.randn(T, 8, d).to(dt), torch.randn(T, 2, d).to(dt)
+    gq, gk = ((1 + 0.2 * torch.randn(d)).to(dt) for _ in range(2))
+    qd, kd = q.cuda(), k.cuda()
+    sx.qk_norm_rope_rows(plan, rows.cuda(), i32([len(x) for x in lists]), 98, qd, kd, gq.cuda(), gk.cuda(), 1e-5)
+    live = pos >= 0
+    for got, src, gam in ((qd, q, gq), (kd, k, gk)):
+        assert torch.equal(got.cpu()[~live], src[~live])
+        want, bound = R.norm_rope(src[live], gam, 1e-5, pos[live], 5e5, True)
+        near(got.cpu()[live], want, bound, dtype)
+    # a smaller bound takes the first rows of every list
+    q2, k2 = q.cuda(), k.cuda()
+    sx.qk_norm_rope_rows(plan, rows.cuda(), i32([len(x) for x in lists]), 3, q2, k2, gq.cuda(), gk.cuda(), 1e-5)
+    first = torch.zeros(T, dtype=torch.bool)
+    for r in range(2):
+        first[[offs[r] + t for t in lists[r][:3]]] = True
+    assert torch.equal(q2.cpu()[first], qd.cpu()[first]) and torch.equal(q2.cpu()[~first], q[~first])
+    assert torch.equal(k2.cpu()[~first], k[~first])
+    plan.close()
+
+
+# ---------------------------------------------------------------- the 4-bit rows and blocks
+
+def hard_rows(g, n, h, d, dt):
+    """Rows with every awkward group: zeros, ties, borders of the scale, the largest and smallest values, NaN, infinity."""
+    x = torch.randn(n, h, d, generator=g) * torch.exp(4 * torch.randn(n, h, 1, generator=g))
+    f = x.view(-1, 32)
+    m = f.shape[0]
+    tie = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -0.75, -1.25, -2.5, -5.0, 6.0, 0.0, -0.0, 4.0])
+    for i, v in enumerate((0.0, 7.0, 7.03125, 3.5, 3.515625, 3.3e38, -3.3e38, 1e-38, 1e-40, 8e-39, 448.0)):
+        if i < m:
+            f[i] *= 1e-3 * abs(v) / f[i].abs().max() if v else 0.0
+            f[i, 5] = v
+    for i in range(11, min(m, 20)):
+        f[i] = torch.cat([tie, tie]) * 2.0 ** (i - 14)
+    if m > 24:
+        f[21, 3], f[22, 31], f[23, 0] = math.nan, math.inf, -math.inf
+    return x.to(dt)
+
+
+@pytest.mark.parametrize("dtype,h,d,n", [("bf16", 8, 128, 1), ("bf16", 2, 64, 16), ("bf16", 1, 128, 37), ("f32", 4, 64, 50),
+                                         ("f32", 3, 128, 19), ("bf16", 4, 64, 129)])
+def test_kv4_write_and_read_rows(dtype, h, d, n):
+    g = torch.Generator().manual_seed(n * d)
+    dt = DT[dtype]
+    k, v = hard_rows(g, n, h, d, dt), hard_rows(g, n, h, d, dt).flip(0)
+    pool = torch.randint(0, 256, (n // 8 + 3, h, R.record(d)), generator=g, dtype=torch.uint8)
+    slots = torch.randperm(pool.shape[0] * 16, generator=g)[:n].int()
+    if n > 5:
+        slots[2], slots[5] = -1, pool.shape[0] * 16      # skipped: none, and behind the pool
+    desc = sx.make_desc(h, h, d, dtype, 1e4)
+    packed = torch.stack([k, v], 1).cuda()                # rows apart
+    pd = pool.cuda()
+    sx.kv4_write(desc, packed[:, 0], packed[:, 1], slots.cuda(), pd)
+    want = pool.clone()
+    kv, vv = R.put_rows(want, k, v, slots)
+    assert torch.equal(pd.cpu(), want)
+    out = torch.full((n, 2, h, d), -7.0, dtype=dt, device="cuda")
+    sx.kv4_read(desc, pd, slots.cuda(), out[:, 0], out[:, 1])
+    live = (slots >= 0) & (slots < pool.shape[0] * 16)
+    for got, exact in ((out[:, 0].cpu(), kv), (out[:, 1].cpu(), vv)):
+        assert torch.equal(got[live].double().nan_to_num(1e300), exact[live].nan_to_num(1e300))
+        assert (got[~live] == -7).all()
+
+
+@pytest.mark.parametrize("dtype,h,d,n", [("bf16", 8, 128, 1), ("bf16", 2, 64, 7), ("f32", 3, 128, 5), ("f32", 1, 64, 11)])
+def test_kv4_pack_and_unpack_blocks(dtype, h, d, n):
+    g = torch.Generator().manual_seed(n + h)
+    dt = DT[dtype]
+    k, v = (hard_rows(g, (n + 2) * 16, h, d, dt).view(n + 2, 16, h, d).transpose(1, 2).contiguous() for _ in range(2))
+    pool = torch.randint(0, 256, (n + 3, h, R.record(d)), generator=g, dtype=torch.uint8)
+    src, mid = torch.randperm(n + 2, generator=g)[:n].int(), torch.randperm(n + 3, generator=g)[:n].int()
+    if n > 4:
+        src[1], mid[3] = -1, n + 3
+    desc = sx.make_desc(h, h, d, dtype, 1e4)
+    pd = pool.cuda()
+    sx.kv4_pack(desc, k.cuda(), v.cuda(), src.cuda(), pd, mid.cuda())
+    want = pool.clone()
+    live = [i for i in range(n) if 0 <= src[i] < n + 2 and 0 <= mid[i] < n + 3]
+    for i in live:
+        R.put_rows(want, k[src[i]].transpose(0, 1), v[src[i]].transpose(0, 1), mid[i] * 16 + torch.arange(16))
+    assert torch.equal(pd.cpu(), want)
+    ko, vo = (torch.full((n + 2, h, 16, d), -7.0, dtype=dt, device="cuda") for _ in range(2))
+    sx.kv4_unpack(desc, pd, mid.cuda(), ko, vo, src.cuda())
+    seen = torch.zeros(n + 2, dtype=torch.bool)
+    for i in live:
+        seen[src[i]] = True
+        for got, x in ((ko, k), (vo, v)):
+            assert torch.equal(got[src[i]].cpu().double().nan_to_num(1e300), R.round4(x[src[i]])[0].nan_to_num(1e300))
+    assert (ko.cpu()[~seen] == -7).all() and (vo.cpu()[~seen] == -7).all()
+
+
+# ---------------------------------------------------------------- attention
+
+class Batch:
+    """Requests of given (query tokens, keys), their blocks shuffled over a pool of random values."""
+
+    def __init__(self, sizes, hq, hkv, d, dtype, seed=0, spare=3, packed=False, width=None):
+        g = torch.Generator().manual_seed(seed)
+        self.nq, self.nk = [s[0] for s in sizes], [s[1] for s in sizes]
+        self.hq, self.hkv, self.d, self.dtype = hq, hkv, d, dtype
+        counts = [-(-n // 16) for n in self.nk]
+        nb = sum(counts) + spare
+        x = torch.randn(nb * 16, hkv, d, generator=g) * torch.exp(0.5 * torch.randn(1, hkv, d, generator=g))
+        y = torch.randn(nb * 16, hkv, d, generator=g)
+        desc = sx.make_desc(hq, hkv, d, "f32", 1e4)
+        self.pool = torch.zeros(nb, hkv, R.record(d), dtype=torch.uint8, device="cuda")
+        sx.kv4_write(desc, x.cuda(), y.cuda(), torch.arange(nb * 16, dtype=torch.int32).cuda(), self.pool)
+        self.table = torch.full((len(sizes), width or max([1] + counts)), -1, dtype=torch.int32)
+        ids, at = torch.randperm(nb, generator=g), 0
+        for r, c in enumerate(counts):
+            self.table[r, :c] = ids[at:at + c]
+            at += c
+        self.cu = [0]
+        for n in self.nq:
+            self.cu.append(self.cu[-1] + n)
+        rows = self.cu[-1] + 2                              # two rows behind the last sequence
+        q = torch.randn(rows, hq + 2 * hkv, d, generator=g).to(DT[dtype])
+        self.q = q[:, :hq].cuda() if not packed else q.cuda()[:, :hq]
+        if not packed:
+            self.q = self.q.contiguous()
+        self.desc = sx.make_desc(hq, hkv, d, dtype, 1e4)
+
+    def run(self, max_q=None, max_keys=None, lse=True, table=None, workspace=None):
+        out = torch.full((self.q.shape[0], self.hq, self.d), -7.0, dtype=DT[self.dtype], device="cuda")
+        ls = torch.full(out.shape[:2], -7.0, device="cuda") if lse else None
+        mq, mk = max_q or max(1, max(self.nq)), max_keys or max(1, max(self.nk))
+        size = sx.kv4_attn_workspace(self.desc, len(self.nq), mq, mk)
+        ws = workspace if workspace is not None else torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+        sx.kv4_attn(self.desc, self.q, i32(self.cu), i32(self.nk), (self.table if table is None else table).cuda(), self.pool,
+                    out, mq, mk, ws, lse=ls)
+        return out, ls
+
+    def check(self, table=None, **kw):
+        out, lse = self.run(table=table, **kw)
+        pool, table = self.pool.cpu(), self.table if table is None else table
+        kv = [R.rows_of(pool, table[r], n, self.d) for r, n in enumerate(self.nk)]
+        want, wl, bound, lb = R.attention(self.q.cpu(), self.cu, self.nk, kv, self.d ** -0.5)
+        n = self.cu[-1]
+        assert (out[n:] == -7).all() and (lse[n:] == -7).all(), "rows behind the last sequence were written"
+        near(out[:n], want[:n], bound[:n], f"out {self.dtype}")
+        gl, wl = lse[:n].double().cpu(), wl[:n]
+        assert torch.equal(gl == -math.inf, wl == -math.inf) and torch.equal(gl.isnan(), wl.isnan())
+        fin = torch.isfinite(wl)
+        assert ((gl - wl).abs()[fin] <= lb[:n][fin]).all(), "lse"
+        return out, lse
+
+
+SHAPES = [(8, 2, 128, "bf16"), (7, 1, 64, "bf16"), (4, 4, 128, "f32"), (14, 2, 64, "f32"), (64, 1, 128, "bf16"), (24, 1, 64, "f32")]
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
+def test_kv4_attn_single_tokens(hq, hkv, d, dtype):
+    sizes = [(1, n) for n in (1, 2, 15, 16, 17, 31, 32, 33, 127, 128, 129, 200, 0, 511, 512, 513, 640, 641, 1030)]
+    Batch(sizes, hq, hkv, d, dtype, seed=d + hq).check()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES)
+def test_kv4_attn_query_runs(hq, hkv, d, dtype):
+    sizes = [(2, 2), (5, 37), (0, 40), (16, 16), (3, 600), (17, 700), (1, 0), (4, 2), (40, 130), (33, 1100)]
+    Batch(sizes, hq, hkv, d, dtype, seed=d * hq, packed=True).check()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,nq,nk", [(8, 2, 128, "bf16", 300, 300), (4, 1, 64, "bf16", 257, 1500), (2, 2, 128, "f32", 130, 1025),
+                                                  (6, 1, 128, "bf16", 700, 900), (1, 1, 64, "f32", 513, 600), (2, 1, 64, "bf16", 90, 20),
+                                                  (5, 1, 128, "bf16", 64, 2000), (16, 1, 128, "bf16", 260, 270)])
+def test_kv4_attn_prompt_chunks(hq, hkv, d, dtype, nq, nk):
+    Batch([(nq, nk), (1, 33), (nq // 3, nk // 2)], hq, hkv, d, dtype, seed=nq).check()
+
+
+def test_kv4_attn_long_axis():
+    # 40000 keys: 64 chunks; a few rows
+    Batch([(1, 40000), (2, 33333)], 4, 1, 64, "bf16", seed=5).check()
+
+
+def test_kv4_attn_missing_and_foreign_blocks():
+    b = Batch([(1, 700), (6, 300), (1, 40), (20, 90)], 8, 2, 128, "bf16", seed=2)
+    t = b.table.clone()
+    t[0, 3], t[0, 40], t[1, 0], t[1, 18], t[3, 2] = -1, b.pool.shape[0], -5, (1 << 31) - 1, -1
+    t[2, :] = -1                                            # nothing of request 2 is there: an empty row
+    out, lse = b.check(table=t)
+    assert (out[b.cu[2]] == 0).all() and (lse[b.cu[2]] == -math.inf).all()
+
+
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f32"), (64, "bf16"), (128, "f32")])
+def test_kv4_attn_nan_stays_where_it_is_seen(d, dtype):
+    # NaN groups in the last block behind the last key, and in keys that only later rows see
+    b = Batch([(9, 41), (1, 30), (70, 95)], 4, 2, d, dtype, seed=d)
+    bad = torch.zeros(1, 2, d, device="cuda")
+    for r, t in ((0, 41), (0, 47), (1, 30), (1, 31), (2, 95)):     # behind the end
+        s = i32([int(b.table[r, t // 16]) * 16 + t % 16])
+        sx.kv4_write(sx.make_desc(2, 2, d, "f32", 1e4), bad + math.nan, bad + math.inf, s, b.pool)
+    out, _ = b.check()
+    assert not out[:b.cu[-1]].isnan().any()
+    one = bad.clone()
+    one[0, 1, d - 32 + 3] = math.nan                       # one group of one head, in a value that rows 35.. see
+    for r, t in ((0, 35), (2, 50)):
+        s = i32([int(b.table[r, t // 16]) * 16 + t % 16])
+        sx.kv4_write(sx.make_desc(2, 2, d, "f32", 1e4), bad + 0.5, one, s, b.pool)
+    out, lse = b.check()
+    nan = out.isnan()
+    assert not nan[:b.cu[1]][: 35 - 32].any() and nan[3, 2:, d - 32:].all() and not nan[3, 2:, :d - 32].any()
+    assert not lse.isnan().any()
+    s = i32([int(b.table[0, 36 // 16]) * 16 + 36 % 16])    # and in a key
+    sx.kv4_write(sx.make_desc(2, 2, d, "f32", 1e4), one, bad, s, b.pool)
+    b.check()
+
+
+def test_kv4_attn_infinite_and_huge_queries():
+    b = Batch([(4, 100), (1, 700)], 4, 2, 128, "f32", seed=8)
+    b.q[0, 0, 3], b.q[4, 2, 0] = math.nan, math.nan
+    b.q[1] *= 1e4                                          # one key takes all the weight
+    b.check()
+
+
+def test_kv4_attn_no_dependence_on_the_batch_or_the_bounds():
+    sizes = [(1, 5), (1, 3000), (7, 900), (1, 640), (90, 1200), (3, 20000)]
+    b = Batch(sizes, 8, 2, 128, "bf16", seed=4)
+    out, lse = b.run()
+    out2, lse2 = b.run(max_q=333, max_keys=60000)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    assert torch.equal(b.run(lse=False)[0], out)
+    for r in range(len(sizes)):
+        o = torch.empty_like(b.q[b.cu[r]:b.cu[r + 1]])
+        ws = torch.empty(sx.kv4_attn_workspace(b.desc, 1, sizes[r][0], sizes[r][1]), dtype=torch.uint8, device="cuda")
+        sx.kv4_attn(b.desc, b.q[b.cu[r]:b.cu[r + 1]], i32([0, sizes[r][0]]), i32([sizes[r][1]]), b.table[r:r + 1].cuda(), b.pool, o,
+                    sizes[r][0], sizes[r][1], ws)
+        assert torch.equal(o, out[b.cu[r]:b.cu[r + 1]]), r
+
+
+def test_kv4_attn_lengths_beyond_the_bounds_are_cut():
+    # the release library never reads past what the host was told: 2 blocks a row, 20 keys, 3 queries
+    b = Batch([(1, 32), (1, 32)], 4, 2, 64, "bf16", seed=3)
+    out = torch.full_like(b.q, -7.0)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    sx.kv4_attn(b.desc, b.q, i32([0, 1, 900]), i32([1 << 30, -4]), b.table.cuda(), b.pool, out, 3, 20, ws)
+    c = Batch([(1, 20), (3, 0)], 4, 2, 64, "bf16", seed=3)
+    c.pool, c.table = b.pool, b.table
+    ref = torch.full_like(b.q, -7.0)
+    sx.kv4_attn(b.desc, b.q, i32([0, 1, 4]), i32([20, 0]), b.table.cuda(), b.pool, ref, 3, 20, ws)
+    assert torch.equal(out, ref)
+
+
+def test_kv4_attn_pool_beyond_32_bits():
+    nb = (5 << 30) // (8 * R.record(128))                   # 5 GiB of 8 heads
+    pool = torch.empty(nb, 8, R.record(128), dtype=torch.uint8, device="cuda")
+    ids = torch.tensor([nb - 1, 3, nb - 200, nb // 2 + 7, nb - 77], dtype=torch.int32)
+    desc = sx.make_desc(16, 8, 128, "bf16", 1e4)
+    k, v = torch.randn(75, 8, 128).bfloat16(), torch.randn(75, 8, 128).bfloat16()
+    slots = ids[torch.arange(75) // 16] * 16 + (torch.arange(75) % 16).int()
+    sx.kv4_write(desc, k.cuda(), v.cuda(), slots.cuda(), pool)
+    ko, vo = torch.empty_like(k).cuda(), torch.empty_like(v).cuda()
+    sx.kv4_read(desc, pool, slots.cuda(), ko, vo)
+    assert torch.equal(ko.cpu().double(), R.round4(k)[0]) and torch.equal(vo.cpu().double(), R.round4(v)[0])
+    q = torch.randn(2, 16, 128).bfloat16().cuda()
+    out = torch.empty_like(q)
+    sx.kv4_attn(desc, q, i32([0, 2]), i32([75]), ids[None].cuda(), pool, out, 2, 75,
+                torch.empty(16, dtype=torch.uint8, device="cuda"))
+    kv = [(ko.cpu().double(), vo.cpu().double(), torch.ones(75, dtype=torch.bool))]
+    want, _, bound, _ = R.attention(q.cpu(), [0, 2], [75], kv, 128 ** -0.5)
+    near(out, want, bound, "bf16")
+
+
+# ---------------------------------------------------------------- together
+
+class Loop:
+    """A decoding loop of one layer: slots, norm and rotation, 4-bit write, attention, all state on the GPU."""
+
+    def __init__(self, ctx, hq, hkv, d, dtype, width, seed):
+        g = torch.Generator().manual_seed(seed)
+        n, dt = len(ctx), DT[dtype]
+        self.hq, self.hkv, self.d, self.n, self.width = hq, hkv, d, n, width
+        self.desc = sx.make_desc(hq, hkv, d, dtype, 1e6)
+        nb = n * width
+        self.pool = torch.zeros(nb, hkv, R.record(d), dtype=torch.uint8, device="cuda")
+        self.free = torch.randperm(nb, generator=g).int().cuda()
+        self.table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+        self.ctx, self.seq = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+        self.head = torch.zeros(2, dtype=torch.int32, device="cuda")
+        self.state = torch.zeros(2, dtype=torch.int32, device="cuda")
+        self.gq, self.gk = ((1 + 0.2 * torch.randn(d, generator=g)).to(dt).cuda() for _ in range(2))
+        self.g, self.dt = g, dt
+        self.rows = []                                     # (positions, rotated k, v) per step, for the reference
+
+    def buffers(self, room, max_q, max_keys):
+        e = lambda *s, t=self.dt: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+        return dict(qkv=e(room, self.hq + 2 * self.hkv, self.d), pos=e(room, t=torch.int32), slot=e(room, t=torch.int32),
+                    cu=e(self.n + 1, t=torch.int32), q=e(room, self.hq, self.d), k=e(room, self.hkv, self.d),
+                    out=e(room, self.hq, self.d), new=e(self.n, t=torch.int32), max_q=max_q, max_keys=max_keys,
+                    ws=e(max(16, sx.kv4_attn_workspace(self.desc, self.n, max_q, max_keys)), t=torch.uint8))
+
+    def step(self, b):
+        hq, hkv = self.hq, self.hkv
+        sx.append_slots(self.ctx, b["new"], self.free, self.table, self.seq, b["cu"], b["pos"], b["slot"], self.state,
+                        free_head=self.head)
+        sx.qk_norm_rope(self.desc, b["qkv"][:, :hq], b["qkv"][:, hq:hq + hkv], b["pos"], b["q"], b["k"], self.gq, self.gk, 1e-6)
+        sx.kv4_write(self.desc, b["k"], b["qkv"][:, hq + hkv:], b["slot"], self.pool)
+        sx.kv4_attn(self.desc, b["q"], b["cu"], self.seq, self.table, self.pool, b["out"], b["max_q"], b["max_keys"], b["ws"])
+        self.ctx.copy_(self.seq)
+        self.head.copy_(self.state)
+
+    def load(self, b, new):
+        b["new"].copy_(torch.tensor(new, dtype=torch.int32))
+        b["qkv"].copy_(torch.randn(b["qkv"].shape, generator=self.g).to(self.dt))
+
+    def reference(self, b, hist, new):
+        """Appends the step's rows to the requests' float64 histories and returns the attention over them."""
+        x, at, kv, lens = b["qkv"].cpu(), 0, [], []
+        hq, hkv = self.hq, self.hkv
+        qs = []
+        for r, n in enumerate(new):
+            pos = torch.arange(n) + sum(len(k) for k in hist[r][0])
+            q, k, v = (x[at:at + n, i:j] for i, j in ((0, hq), (hq, hq + hkv), (hq + hkv, hq + 2 * hkv)))
+            qs.append(R.norm_rope(q, self.gq.cpu(), 1e-6, pos, 1e6, True)[0])
+            # the library's own rotated rows, checked by their own test, so that a rounding next to a border of the
+            # 4-bit format is not counted here
+            hist[r][0].append(R.round4(b["k"][at:at + n].cpu())[0])
+            hist[r][1].append(R.round4(v)[0])
+            k, v = torch.cat(hist[r][0]), torch.cat(hist[r][1])
+            kv.append((k, v, torch.ones(len(k), dtype=torch.bool)))
+            lens.append(len(k))
+            at += n
+        cu = [sum(new[:r]) for r in range(len(new) + 1)]
+        q = torch.cat(qs)
+        got_q = b["q"][:at].cpu()
+        near(got_q, q, torch.full_like(q, 2.0 ** -18) * q.abs().amax(), "bf16" if self.dt is torch.bfloat16 else "f32")
+        return at, R.attention(got_q, cu, lens, kv, self.d ** -0.5)
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 2, 128, "bf16"), (6, 2, 64, "f32")])
+def test_prompt_then_decoding_steps(hq, hkv, d, dtype):
+    ctx = [0, 0, 0, 0]
+    loop = Loop(ctx, hq, hkv, d, dtype, 48, seed=d)
+    hist = [([], []) for _ in ctx]
+    steps = [[70, 3, 0, 600], [1, 1, 20, 1], [1, 1, 1, 1], [1, 0, 1, 5], [1, 1, 1, 1]]
+    for i, new in enumerate(steps):
+        log("step", i, new)
+        b = loop.buffers(sum(new) + i, max(new), 48 * 16)
+        loop.load(b, new)
+        loop.step(b)
+        n, (want, _, bound, _) = loop.reference(b, hist, new)
+        near(b["out"][:n], want, bound, dtype)
+        assert (b["out"][n:] == 0).all() and loop.state[1].item() == 0
+
+
+def test_decoding_in_a_graph():
+    # one captured step replayed with the state on the GPU, against the same steps run eagerly; eager work and
+    # synchronisations stand between the replays, and a second graph shares nothing but the library
+    def fresh():
+        loop = Loop([0] * 5, 8, 2, 128, "bf16", 80, seed=11)
+        b = loop.buffers(5 * 90, 90, 80 * 16)
+        loop.load(b, [90, 1, 33, 64, 80])
+        loop.step(b)
+        return loop, loop.buffers(7, 1, 80 * 16)
+
+    (eager, be), (one, b1), (two, b2) = fresh(), fresh(), fresh()
+    graphs = []
+    for loop, b in ((one, b1), (two, b2)):
+        keep = [x.clone() for x in (loop.ctx, loop.seq, loop.head, loop.state, loop.table, loop.pool)]
+        b["new"].fill_(1)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            loop.step(b)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            loop.step(b)
+        for x, y in zip((loop.ctx, loop.seq, loop.head, loop.state, loop.table, loop.pool), keep):
+            x.copy_(y)
+        graphs.append(graph)
+    g = torch.Generator().manual_seed(3)
+    for i in range(40):
+        x = torch.randn(b1["qkv"].shape, generator=g).bfloat16()
+        for b in (be, b1, b2):
+            b["qkv"].copy_(x)
+        be["new"].fill_(1)
+        eager.step(be)
+        graphs[0].replay()
+        if i % 7 == 0:
+            torch.cuda.synchronize()
+        graphs[1].replay()
+        for b, loop in ((b1, one), (b2, two)):
+            for n in ("out", "pos", "slot", "cu"):
+                assert torch.equal(b[n], be[n]), (i, n)
+            assert torch.equal(loop.pool, eager.pool) and torch.equal(loop.table, eager.table)
+
+
+def test_two_streams_with_their_own_workspaces():
+    b = Batch([(1, 9000), (4, 2000), (1, 700)], 8, 2, 128, "bf16", seed=6)
+    want = b.run()[0]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    size = sx.kv4_attn_workspace(b.desc, 3, 4, 9000)
+    outs = [torch.empty_like(want) for _ in range(2)]
+    args = [(i32(b.cu), i32(b.nk), b.table.cuda(), torch.empty(size, dtype=torch.uint8, device="cuda")) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, o, (cu, nk, t, ws) in zip(streams, outs, args):
+            sx.kv4_attn(b.desc, b.q, cu, nk, t, b.pool, o, 4, 9000, ws, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o[:b.cu[-1]], want[:b.cu[-1]])
+
+
+def test_packed_prefill_cache_serves_decoding_and_realignment():
+    # the plan's paged cache goes into 4-bit blocks; a token attends over them, and the same blocks, unpacked, are the
+    # source of a re-alignment
+    w = W.custom_workload([[(40, False, 0, None), (60, True, 300, None), (28, False, 0, None)]], n_q_heads=8, n_kv_heads=2,
+                          head_dim=128, dtype="bf16", rope_base=5e5, seed=3, name="pack")
+    t = {n: torch.from_numpy(x).cuda().bfloat16() for n, x in W.layer_tensors(w, 0).items()}
+    plan = sx.Plan(desc_of(w), w.requests, w.n_dst_blocks, w.n_src_blocks)
+    shape = (w.n_dst_blocks, 2, 16, 128)
+    kc, vc = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sx.rope_realign(plan, t["k_src"], t["v_src"], kc, vc)
+    rows, n, m = plan.nonreused_rows()
+    sx.kv_scatter(plan, t["k"], t["v"], kc, vc, rows=rows, n_rows=n, max_rows=m)
+    blocks = torch.as_tensor(list(w.requests[0].block_table), dtype=torch.int32).cuda()
+    pool = torch.zeros(len(blocks) + 2, 2, R.record(128), dtype=torch.uint8, device="cuda")
+    mine = torch.randperm(len(blocks) + 2)[:len(blocks)].int().cuda()
+    desc = desc_of(w)
+    sx.kv4_pack(desc, kc, vc, blocks, pool, mine)
+    q = torch.randn(1, 8, 128, device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    T = w.total_tokens
+    sx.kv4_attn(desc, q, i32([0, 1]), i32([T]), mine[None].contiguous(), pool, out, 1, T, torch.empty(16, dtype=torch.uint8, device="cuda"))
+    dense = [x[blocks.long()].transpose(1, 2).reshape(-1, 2, 128)[:T].cpu() for x in (kc, vc)]
+    kv = [tuple(R.round4(x)[0] for x in dense) + (torch.ones(T, dtype=torch.bool),)]
+    want, _, bound, _ = R.attention(q.cpu(), [0, 1], [T], kv, 128 ** -0.5)
+    near(out, want, bound, "bf16")
+    ks, vs = (torch.zeros((w.n_src_blocks, 2, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    src = torch.arange(w.n_src_blocks, dtype=torch.int32).cuda()
+    pool2 = torch.zeros(w.n_src_blocks, 2, R.record(128), dtype=torch.uint8, device="cuda")
+    sx.kv4_pack(desc, t["k_src"].contiguous(), t["v_src"].contiguous(), src, pool2, src)
+    sx.kv4_unpack(desc, pool2, src, ks, vs, src)
+    assert torch.equal(ks.cpu().double(), R.round4(t["k_src"].cpu())[0])
+    k2, v2 = torch.zeros_like(kc), torch.zeros_like(vc)
+    sx.rope_realign(plan, ks, vs, k2, v2)
+    k3, v3 = torch.zeros_like(kc), torch.zeros_like(vc)
+    sx.rope_realign(plan, R.round4(t["k_src"].cpu())[0].bfloat16().cuda(), R.round4(t["v_src"].cpu())[0].bfloat16().cuda(), k3, v3)
+    assert torch.equal(k2, k3) and torch.equal(v2, v3)
+    plan.close()
+
+
+def test_checked_library_refuses_bad_index_arrays():
+    sx.use_checked(True)
+    try:
+        b = Batch([(1, 30), (2, 40)], 4, 2, 64, "bf16", seed=1)
+
+        def bad(f, text):
+            with pytest.raises(sx.SxError) as e:
+                f()
+            assert e.value.status == sx.SX_EDEVICE and text in str(e.value)
+
+        def attn(cu=b.cu, nk=b.nk, table=b.table):
+            sx.kv4_attn(b.desc, b.q, i32(cu), i32(nk), table.cuda(), b.pool, torch.empty_like(b.q), 2, 40,
+                        torch.empty(16, dtype=torch.uint8, device="cuda"))
+        attn()
+        bad(lambda: attn(cu=[1, 1, 3]), "cu_q[0]")
+        bad(lambda: attn(cu=[0, 1, 4]), "max_q")
+        bad(lambda: attn(nk=[30, 41]), "length")
+        t = b.table.clone()
+        t[1, 2] = b.pool.shape[0]
+        bad(lambda: attn(table=t), "table")
+        k = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+        bad(lambda: sx.kv4_write(b.desc, k, k, i32([0, b.pool.shape[0] * 16]), b.pool), "index")
+        bad(lambda: sx.kv4_read(b.desc, b.pool, i32([-2, 0]), k, k), "index")
+        with pytest.raises(sx.SxError) as e:
+            z = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+            sx.append_slots(i32([3, -1]), None, i32([4, 5]), z(4).view(2, 2), z(2), z(3), z(2), z(2), z(2))
+        assert e.value.status == sx.SX_EDEVICE
+    finally:
+        sx.use_checked(False)
