@@ -9,6 +9,8 @@
 // LDS until the waves of a workgroup, which take the steps of a chunk of keys in turn, add up their parts.
 // Softmax statistics and sums are float32; a probability goes into the product as two bfloat16 parts (float32
 // q: three, and q itself in three), so what is lost there is below the rounding of the output.
+#include <type_traits>
+
 #include "sx_kv4_device.h"
 
 namespace sx {
@@ -97,26 +99,26 @@ struct Page {
     const float s = kv4_scale(ks);
     return as_bf16x8(kv4_pair<0>(k[c], s), kv4_pair<1>(k[c], s), kv4_pair<2>(k[c], s), kv4_pair<3>(k[c], s));
   }
-  // V of the lane's four tokens: w[token][pair of columns]
-  __device__ __forceinline__ void values(uint32_t (&w)[4][D / 32]) const {
+  // V of the lane's four tokens, columns 2 B and 2 B + 1 of the column group
+  template <int B>
+  __device__ __forceinline__ void value_pair(uint32_t (&w)[4]) const {
     const float s[4] = {kv4_scale(vs & 0xff), kv4_scale(vs >> 8 & 0xff), kv4_scale(vs >> 16 & 0xff), kv4_scale(vs >> 24)};
     if constexpr (D == 128) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i][0] = kv4_pair<0>(v[i], s[i]);
-        w[i][1] = kv4_pair<1>(v[i], s[i]);
-        w[i][2] = kv4_pair<2>(v[i], s[i]);
-        w[i][3] = kv4_pair<3>(v[i], s[i]);
-      }
+      for (int i = 0; i < 4; ++i) w[i] = kv4_pair<B>(v[i], s[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
-        w[i][0] = kv4_pair<0>(v[i / 2], s[i]);
-        w[i][1] = kv4_pair<1>(v[i / 2], s[i]);
-        w[i + 1][0] = kv4_pair<2>(v[i / 2], s[i + 1]);
-        w[i + 1][1] = kv4_pair<3>(v[i / 2], s[i + 1]);
+        w[i] = kv4_pair<B>(v[i / 2], s[i]);
+        w[i + 1] = kv4_pair<B + 2>(v[i / 2], s[i + 1]);
       }
     }
+  }
+  // a NaN group's scale as 1 (its codes are zero)
+  __device__ __forceinline__ void drop_bad_values() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((vs >> (8 * i) & 0xff) == 0xff) vs = (vs & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
   }
   // a NaN group among the values of the lane's tokens
   __device__ __forceinline__ bool bad_values() const {
@@ -139,12 +141,28 @@ struct Request {
   }
 };
 
+// Halves of the pairs (x: one of two keys, y: the other) as the two keys of one column: the low or high ones.
+template <int ODD>
+__device__ __forceinline__ uint32_t halves(uint32_t x, uint32_t y) {
+  return __builtin_amdgcn_perm(y, x, ODD ? 0x07060302u : 0x05040100u);
+}
+
+// for_each<N>(f): f(integral constant 0) .. f(N - 1)
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void for_each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    for_each<N, I + 1>(f);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
-// One workgroup: 16 rows of one KV head over one chunk of keys, its NW waves taking steps of two blocks in
-// turn.  Writes the rows' results, or their parts where the request's keys are split.
+// Few query rows: one workgroup takes 16 MT rows of one KV head over one chunk of keys, its NW waves steps of
+// two blocks in turn; the next step's codes are loaded while a step is computed, the block ids of 32 steps at
+// once.  Writes the rows' results, or their parts where the request's keys are split.
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW * 64) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+template <typename T, int D, int MT, int NW>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
   constexpr int NC = D / 32;                  // 32-element pieces of a row
   constexpr int NU = D / 16;                  // 16-column tiles of V
   constexpr int NQ = sizeof(T) == 4 ? 3 : 1;  // bfloat16 parts of a query element, and of a probability
@@ -157,179 +175,217 @@ __global__ __launch_bounds__(NW * 64) void kv4_attn_kernel(Kv4AttnK a, int tiles
   idx /= a.Hkv;
   const int c = idx / tiles, tile = idx % tiles, r = blockIdx.y;   // (chunks slowest, as below)
   const Request q(a, r);
-  const int row0 = tile * 16;
+  const int row0 = tile * 16 * MT;
   if (row0 >= q.rows || c >= q.split.n || (sizeof(T) == 2 && q.rows > kKv4FewRows)) return;
   const int G = a.Hq / a.Hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row = min(row0 + (lane & 15), q.rows - 1), lg = lane >> 4;
-  const int lim = q.off + row / G;            // last key that this lane's row sees
-  const int lim_min = q.off + row0 / G, lim_max = q.off + min(row0 + 15, q.rows - 1) / G;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lg = lane >> 4;
+  int row[MT], lim[MT];                       // this lane's rows, and the last key each sees
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    row[t] = min(row0 + 16 * t + (lane & 15), q.rows - 1);
+    lim[t] = q.off + row[t] / G;
+  }
+  const int lim_min = q.off + row0 / G, lim_max = q.off + min(row0 + 16 * MT - 1, q.rows - 1) / G;
   const int k0 = c * q.split.keys;            // (c < n: below len)
-  const int k1 = min(min(k0 + (int64_t)q.split.keys, (int64_t)q.len), (int64_t)lim_max + 1);
+  const int k1 = (int)min(min(k0 + (int64_t)q.split.keys, (int64_t)q.len), (int64_t)lim_max + 1);
   const int32_t* table = a.table + (int64_t)r * a.max_blocks;
+  const uint8_t* pool = a.pool + (int64_t)h * kv4_record(D);
+  const int64_t block_bytes = (int64_t)a.Hkv * kv4_record(D);
 
-  bf16x8_t qf[NC][NQ];
-  {
-    const T* src = (const T*)a.q + (int64_t)(q.q0 + row / G) * a.q_ld + (h * G + row % G) * D + lg * (D / 4);
+  // this wave's steps: keys k0 + 32 (wave + NW i) ..; block ids of steps 32 run .. + 31, two a step
+  const int steps = k1 > k0 ? ((k1 - k0 + 31) / 32 - wave + NW - 1) / NW : 0;
+  auto load_ids = [&](int run) {
+    const int page = k0 / kBlock + 2 * (wave + NW * (32 * run + (lane >> 1))) + (lane & 1);
+    const int id = (int64_t)page * kBlock < k1 ? table[page] : -1;
+    return id < a.n_blocks ? id : -1;
+  };
+  int ids = load_ids(0);
+  Page<D> next[2];
+  int next_id[2];
+  auto fetch = [&](int i) {
+    if (i > 0 && (i & 31) == 0) ids = load_ids(i >> 5);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      next_id[j] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + j);
+      if (next_id[j] >= 0) next[j].load(pool + next_id[j] * block_bytes, lane);
+      else next[j].clear();
+    }
+  };
+  if (steps > 0) fetch(0);
+
+  bf16x8_t qf[MT][NC][NQ];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const T* src = (const T*)a.q + (int64_t)(q.q0 + row[t] / G) * a.q_ld + (h * G + row[t] % G) * D + lg * (D / 4);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       if constexpr (NQ == 1) {
-        qf[i][0] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + i * 8));
+        qf[t][i][0] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + i * 8));
       } else {
         float x[8];
         load8(src + i * 8, x);
-        split_parts<NQ>(x, qf[i]);
+        split_parts<NQ>(x, qf[t][i]);
       }
     }
   }
-  f32x4_t o[NU];
+  f32x4_t o[MT][NU];
+  float m[MT], l[MT];
 #pragma unroll
-  for (int u = 0; u < NU; ++u) o[u] = (f32x4_t){0, 0, 0, 0};
-  float m = kNegInf, l = 0.0f;
+  for (int t = 0; t < MT; ++t) {
+    m[t] = kNegInf;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) o[t][u] = (f32x4_t){0, 0, 0, 0};
+  }
 
-  for (int kb = k0 + wave * 32; kb < k1; kb += NW * 32) {
-    Page<D> pg[2];
-    bool have[2];
+  for (int i = 0; i < steps; ++i) {
+    const int kb = k0 + 32 * (wave + NW * i);
+    Page<D> pg[2] = {next[0], next[1]};
+    const int id[2] = {next_id[0], next_id[1]};
+    if (i + 1 < steps) fetch(i + 1);
+    if (kb + 32 > q.len) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int p = kb / kBlock + j;
-      const int id = p * kBlock < k1 ? table[p] : -1;
-      have[j] = id >= 0 && id < a.n_blocks;
-      if (have[j]) pg[j].load(a.pool + ((int64_t)id * a.Hkv + h) * kv4_record(D), lane);
-      else pg[j].clear();
-      if ((p + 1) * kBlock > q.len) pg[j].drop_values_from(q.len - p * kBlock, lane);
+      for (int j = 0; j < 2; ++j) pg[j].drop_values_from(q.len - kb - 16 * j, lane);
     }
-    float s[8];
+    f32x4_t sc[MT][2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      f32x4_t acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const bf16x8_t kf = pg[j].k_part(i);
+      for (int t = 0; t < MT; ++t) sc[t][j] = (f32x4_t){0, 0, 0, 0};
 #pragma unroll
-        for (int n = NQ - 1; n >= 0; --n) acc = mfma16(kf, qf[i][n], acc);
+      for (int n = 0; n < NC; ++n) {
+        const bf16x8_t kf = pg[j].k_part(n);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int p = NQ - 1; p >= 0; --p) sc[t][j] = mfma16(kf, qf[t][n][p], sc[t][j]);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * j + i] = acc[i];
     }
     const bool edge = kb + 31 > lim_min;       // some row does not see every key of the step
-    if (edge || !have[0] || !have[1]) {
+    bf16x8_t pf[MT][NP];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+    for (int t = 0; t < MT; ++t) {
+      float s[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!have[j] || kb + 16 * j + 4 * lg + i > lim) s[4 * j + i] = kNegInf;
+      for (int e = 0; e < 8; ++e) s[e] = sc[t][e >> 2][e & 3];
+      if (edge || id[0] < 0 || id[1] < 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (id[e >> 2] < 0 || kb + 16 * (e >> 2) + 4 * lg + (e & 3) > lim[t]) s[e] = kNegInf;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mn = fmaxf(m[t], top * a.scale);
+      const float base = mn == kNegInf ? 0.0f : mn;
+      if (__any(mn > m[t])) {
+        const float f = __builtin_amdgcn_exp2f(m[t] - base);
+        l[t] *= f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) o[t][u] *= f;
+        m[t] = mn;
+      }
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -base));
+        l[t] += p[e];
+      }
+      split_parts<NP>(p, pf[t]);
     }
-    float top = s[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float mn = fmaxf(m, top * a.scale);
-    const float base = mn == kNegInf ? 0.0f : mn;
-    if (__any(mn > m)) {
-      const float f = __builtin_amdgcn_exp2f(m - base);
-      l *= f;
-#pragma unroll
-      for (int u = 0; u < NU; ++u) o[u] *= f;
-      m = mn;
-    }
-    float p[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale, -base));
-      l += p[i];
-    }
-    bf16x8_t pf[NP];
-    split_parts<NP>(p, pf);
     // a NaN group among the values of keys that some rows see and some do not: these rows get it, the others
     // nothing
     if (edge && __any(pg[0].bad_values() || pg[1].bad_values())) {
-      float nan = 0.0f;
       const int grp = lg * (D / 4) / kKv4Group;   // of the output elements that this lane holds
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int pbase = kb + 16 * j;
-        if (have[j]) {
-          const uint8_t* sc = a.pool + ((int64_t)table[pbase / kBlock] * a.Hkv + h) * kv4_record(D) + kv4_v_scales(D) + grp * 16;
-          for (int t = 0; t < 16 && pbase + t < q.len; ++t)
-            if (sc[t] == 255 && pbase + t <= lim) nan = __builtin_nanf("");
+      for (int t = 0; t < MT; ++t) {
+        float nan = 0.0f;
+        for (int k = kb; k < min(kb + 32, q.len); ++k) {
+          const int b = (k - kb) >> 4;
+          if (id[b] >= 0 && k <= lim[t] && pool[id[b] * block_bytes + kv4_v_scales(D) + grp * 16 + (k & 15)] == 255)
+            nan = __builtin_nanf("");
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((pg[j].vs >> (8 * i) & 0xff) == 0xff) {
-            pg[j].vs = (pg[j].vs & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));   // (its codes are zero)
-          }
+        for (int u = 0; u < NU; ++u) o[t][u] += nan;
       }
-#pragma unroll
-      for (int u = 0; u < NU; ++u) o[u] += nan;
+      pg[0].drop_bad_values();
+      pg[1].drop_bad_values();
     }
-    uint32_t w0[4][NC], w1[4][NC];
-    pg[0].values(w0);
-    pg[1].values(w1);
+    for_each<NC>([&](auto bc) {
+      constexpr int B = decltype(bc)::value;
+      uint32_t w0[4], w1[4];
+      pg[0].template value_pair<B>(w0);
+      pg[1].template value_pair<B>(w1);
+      for_each<2>([&](auto odd) {
+        constexpr int O = decltype(odd)::value, u = 2 * B + O;
+        const bf16x8_t vf = as_bf16x8(halves<O>(w0[0], w0[1]), halves<O>(w0[2], w0[3]), halves<O>(w1[0], w1[1]),
+                                      halves<O>(w1[2], w1[3]));
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      // element u of every token: the low or high half of its pair u / 2
-      const uint32_t sel = u % 2 ? 0x07060302u : 0x05040100u;
-      const int b = u / 2;
-      const bf16x8_t vf = as_bf16x8(__builtin_amdgcn_perm(w0[1][b], w0[0][b], sel), __builtin_amdgcn_perm(w0[3][b], w0[2][b], sel),
-                                    __builtin_amdgcn_perm(w1[1][b], w1[0][b], sel), __builtin_amdgcn_perm(w1[3][b], w1[2][b], sel));
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int n = NP - 1; n >= 0; --n) o[u] = mfma16(vf, pf[n], o[u]);
-    }
+          for (int n = NP - 1; n >= 0; --n) o[t][u] = mfma16(vf, pf[t][n], o[t][u]);
+      });
+    });
   }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
 
-  // the waves' parts: lane l holds row l % 16, columns D / 4 (l / 16) + (D / 16) i + u
-  {
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    // the waves' parts: lane l holds row l % 16, columns D / 4 (l / 16) + (D / 16) i + u
+    if (t > 0) __syncthreads();
+    float lw = l[t];
+    lw += __shfl_xor(lw, 16, 64);
+    lw += __shfl_xor(lw, 32, 64);
     float* dst = &so[wave][lane & 15][lg * (D / 4)];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int u = 0; u < NU; u += 4)
-        *(float4*)(dst + i * NU + u) = make_float4(o[u][i], o[u + 1][i], o[u + 2][i], o[u + 3][i]);
+        *(float4*)(dst + i * NU + u) = make_float4(o[t][u][i], o[t][u + 1][i], o[t][u + 2][i], o[t][u + 3][i]);
     if (lg == 0) {
-      sm[wave][lane & 15] = m;
-      sl[wave][lane & 15] = l;
+      sm[wave][lane & 15] = m[t];
+      sl[wave][lane & 15] = lw;
     }
-  }
-  __syncthreads();
-  constexpr int TPR = NW * 64 / 16;           // threads per row
-  constexpr int EPT = D / TPR;                // elements per thread
-  const int rr = tid / TPR, d0 = tid % TPR * EPT;
-  if (row0 + rr >= q.rows) return;
-  float mt = sm[0][rr];
+    __syncthreads();
+    constexpr int TPR = NW * 64 / 16;           // threads per row
+    constexpr int EPT = D / TPR;                // elements per thread
+    const int rr = tid / TPR, d0 = tid % TPR * EPT;
+    const int orow = row0 + 16 * t + rr;
+    if (orow >= q.rows) continue;
+    float mt = sm[0][rr];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][rr]);
-  const float base = mt == kNegInf ? 0.0f : mt;
-  float lt = 0.0f, acc[EPT];
+    for (int w = 1; w < NW; ++w) mt = fmaxf(mt, sm[w][rr]);
+    const float base = mt == kNegInf ? 0.0f : mt;
+    float lt = 0.0f, acc[EPT];
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) acc[e] = 0.0f;
+    for (int e = 0; e < EPT; ++e) acc[e] = 0.0f;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const float f = __builtin_amdgcn_exp2f(sm[w][rr] - base);
-    lt = __builtin_fmaf(sl[w][rr], f, lt);
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][rr] - base);
+      lt = __builtin_fmaf(sl[w][rr], f, lt);
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) acc[e] = __builtin_fmaf(so[w][rr][d0 + e], f, acc[e]);
-  }
-  const int orow = row0 + rr;
-  if (q.split.n == 1) {
-    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-    const int64_t at = (int64_t)(q.q0 + orow / G) * a.Hq + h * G + orow % G;
-    T* dst = (T*)a.out + at * D + d0;
-#pragma unroll
-    for (int e = 0; e < EPT; e += 2) {
-      if constexpr (sizeof(T) == 2) *(uint32_t*)(dst + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
-      else *(float2*)(dst + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
+      for (int e = 0; e < EPT; ++e) acc[e] = __builtin_fmaf(so[w][rr][d0 + e], f, acc[e]);
     }
-    if (a.lse && d0 == 0) a.lse[at] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
-  } else {
-    const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + (int64_t)c * q.rows + orow;
-    float* dst = a.part + at * D + d0;
+    if (q.split.n == 1) {
+      const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+      const int64_t at = (int64_t)(q.q0 + orow / G) * a.Hq + h * G + orow % G;
+      T* dst = (T*)a.out + at * D + d0;
 #pragma unroll
-    for (int e = 0; e < EPT; e += 2) *(float2*)(dst + e) = make_float2(acc[e], acc[e + 1]);
-    if (d0 == 0) a.part_ml[at] = make_float2(mt, lt);
+      for (int e = 0; e < EPT; e += 2) {
+        if constexpr (sizeof(T) == 2) *(uint32_t*)(dst + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
+        else *(float2*)(dst + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
+      }
+      if (a.lse && d0 == 0) a.lse[at] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
+    } else {
+      const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + (int64_t)c * q.rows + orow;
+      float* dst = a.part + at * D + d0;
+#pragma unroll
+      for (int e = 0; e < EPT; e += 2) *(float2*)(dst + e) = make_float2(acc[e], acc[e + 1]);
+      if (d0 == 0) a.part_ml[at] = make_float2(mt, lt);
+    }
   }
 }
 
@@ -454,23 +510,19 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int t
       }
       if (key + kBlock > q.len) p.drop_values_from(q.len - key, lane);
       if (k0 + t * kWideKeys + kWideKeys - 1 > lim0) {   // some row does not see every key of the tile
-        const bool bad = p.bad_values();
-        if (__any(bad)) {
+        if (__any(p.bad_values())) {
           if (lane == 0) s_nan[buf] = 1;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if ((p.vs >> (8 * i) & 0xff) == 0xff) p.vs = (p.vs & ~(0xffu << (8 * i))) | (0x7fu << (8 * i));
+          p.drop_bad_values();
         }
       }
-      uint32_t w[4][ND];
-      p.values(w);
       char* dst = smem + (NBUF + buf) * TILEB + sj * ND * 1024 + ((lg & 1) * 32 + tok) * 16 + (lg >> 1) * 8;
-#pragma unroll
-      for (int u = 0; u < 2 * ND; ++u) {
-        const uint32_t sel = u % 2 ? 0x07060302u : 0x05040100u;
-        *(uint2*)(dst + u / 2 * 1024 + u % 2 * 256) = make_uint2(__builtin_amdgcn_perm(w[1][u / 2], w[0][u / 2], sel),
-                                                                __builtin_amdgcn_perm(w[3][u / 2], w[2][u / 2], sel));
-      }
+      for_each<ND>([&](auto bc) {
+        constexpr int B = decltype(bc)::value;
+        uint32_t w[4];
+        p.template value_pair<B>(w);
+        *(uint2*)(dst + B * 1024) = make_uint2(halves<0>(w[0], w[1]), halves<0>(w[2], w[3]));
+        *(uint2*)(dst + B * 1024 + 256) = make_uint2(halves<1>(w[0], w[1]), halves<1>(w[2], w[3]));
+      });
     } else {
       if (there) {
 #pragma unroll
@@ -643,38 +695,57 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int t
   }
 }
 
-// The parts of split requests, chunk after chunk: one wave per row.
+// The parts of split requests: one workgroup per row, its four waves the chunks w, w + 4, ... in turn (their
+// loads all in flight at once), then the waves in order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
+  constexpr int E = D / 64;                  // elements per lane
+  constexpr int PER = kKv4Splits / 4;        // most chunks per wave
+  __shared__ float so[4][D];
   const int r = blockIdx.y, h = blockIdx.x % a.Hkv;
   const Request q(a, r);
   if (q.split.n == 1) return;
-  const int G = a.Hq / a.Hkv, lane = threadIdx.x & 63, n = q.split.n;   // n <= 64: a chunk per lane
-  for (int row = blockIdx.x / a.Hkv * 4 + (threadIdx.x >> 6); row < q.rows; row += gridDim.x / a.Hkv * 4) {
+  const int G = a.Hq / a.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = q.split.n;   // n <= 64: a chunk per lane
+  for (int row = blockIdx.x / a.Hkv; row < q.rows; row += gridDim.x / a.Hkv) {
     const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + row;
     const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);
+    float x[PER][E];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 4 * i + wave;
+      const float* src = a.part + (at + (int64_t)c * q.rows) * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[i][e] = c < n ? src[e] : 0.0f;
+    }
     const float mt = wave_max(ml.x);
     const float base = mt == kNegInf ? 0.0f : mt;
     const float f = __builtin_amdgcn_exp2f(ml.x - base);
-    float lt = 0.0f, acc[D / 64];
+    float lt = ml.y * f;                     // (a fixed tree over the lanes)
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] = 0.0f;
-    for (int c = 0; c < n; ++c) {
-      const float fc = __shfl(f, c, 64);
-      lt = __builtin_fmaf(__shfl(ml.y, c, 64), fc, lt);
-      const float* src = a.part + (at + (int64_t)c * q.rows) * D + lane * (D / 64);
+    for (int s = 1; s < 64; s <<= 1) lt += __shfl_xor(lt, s, 64);
+    float acc[E];
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) acc[e] = __builtin_fmaf(src[e], fc, acc[e]);
+    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float fc = __shfl(f, 4 * i + wave, 64);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x[i][e], 4 * i + wave < n ? fc : 0.0f, acc[e]);
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) so[wave][lane * E + e] = acc[e];
+    __syncthreads();
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
     const int64_t to = (int64_t)(q.q0 + row / G) * a.Hq + h * G + row % G;
-    T* dst = (T*)a.out + to * D + lane * (D / 64);
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) {
-      if constexpr (sizeof(T) == 2) dst[e] = (uint16_t)pack_bf16x2(acc[e] * inv, 0.0f);
-      else dst[e] = acc[e] * inv;
+    if (threadIdx.x < D / 2) {
+      const int d = threadIdx.x * 2;
+      const float u = (so[0][d] + so[1][d]) + (so[2][d] + so[3][d]), v = (so[0][d + 1] + so[1][d + 1]) + (so[2][d + 1] + so[3][d + 1]);
+      T* dst = (T*)a.out + to * D + d;
+      if constexpr (sizeof(T) == 2) *(uint32_t*)dst = pack_bf16x2(u * inv, v * inv);
+      else *(float2*)dst = make_float2(u * inv, v * inv);
     }
-    if (a.lse && lane == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
+    if (a.lse && threadIdx.x == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
+    __syncthreads();
   }
 }
 
@@ -692,12 +763,16 @@ static hipError_t launch_kv4(const Kv4AttnK& a, hipStream_t s) {
     }
   }
   const int64_t few = sizeof(T) == 2 && rows > kKv4FewRows ? kKv4FewRows : rows;
-  const int tiles = (int)((few + 15) / 16);
-  hipLaunchKernelGGL((kv4_attn_kernel<T, D, 4>), dim3((unsigned)(tiles * splits * a.Hkv), (unsigned)a.n_req), dim3(256), 0, s,
-                     a, tiles);
+  if (few <= 16) {
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 1, 4>), dim3((unsigned)(splits * a.Hkv), (unsigned)a.n_req), dim3(256), 0, s, a, 1);
+  } else {
+    const int tiles = (int)((few + 31) / 32);
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 4>), dim3((unsigned)(tiles * splits * a.Hkv), (unsigned)a.n_req), dim3(256), 0, s,
+                       a, tiles);
+  }
   if (splits > 1) {
     const int64_t part = rows < kKv4PartRows ? rows : kKv4PartRows;
-    const unsigned wgs = (unsigned)((part + 3) / 4 < 64 ? (part + 3) / 4 : 64);
+    const unsigned wgs = (unsigned)(part < 64 ? part : 64);
     hipLaunchKernelGGL((kv4_merge_kernel<T, D>), dim3(wgs * a.Hkv, (unsigned)a.n_req), dim3(256), 0, s, a);
   }
   return hipGetLastError();
