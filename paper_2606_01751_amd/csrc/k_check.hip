@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void check_kv4_kernel(Kv4AttnK a) {   // one w
     if (r == 0 && a.cu[0] != 0) report_bad(kCuStart, 0, 0, a.cu[0]);
     if (n < 0 || n > a.max_q) report_bad(kCuLength, r, r, n);
     if (r == a.n_req - 1 && a.cu[r + 1] > a.total_q) report_bad(kCuEnd, r, r + 1, a.cu[r + 1]);
-    if (len < 0 || len > a.max_seqlen || len > (int64_t)a.max_blocks * kBlock) report_bad(kBadLength, r, r, len);
+    if (len < 0 || len > a.max_keys) report_bad(kBadLength, r, r, len);
   }
   const int64_t blocks = min(((int64_t)max(len, 0) + kBlock - 1) / kBlock, (int64_t)a.max_blocks);
   for (int64_t i = threadIdx.x; i < blocks; i += 256) {

@@ -35,9 +35,9 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// A float32 as a sum of N bfloat16 parts, each the rounding of what the others leave (an infinity or NaN
-// stands in the first alone): part i of x[0..8).
-template <int N>
+// A float32 as a sum of N bfloat16 parts, each the rounding of what the others leave: part i of x[0..8).  FINITE:
+// no infinities among them (otherwise one stands in the first part alone).
+template <int N, bool FINITE = false>
 __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part)[N]) {
   float rest[8];
 #pragma unroll
@@ -51,8 +51,8 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part
 #pragma unroll
     for (int e = 0; e < 4 && i + 1 < N; ++e) {
       const float lo = bf16_lo(w[e]), hi = bf16_hi(w[e]);
-      rest[2 * e] = __builtin_isfinite(lo) ? rest[2 * e] - lo : 0.0f;
-      rest[2 * e + 1] = __builtin_isfinite(hi) ? rest[2 * e + 1] - hi : 0.0f;
+      rest[2 * e] = FINITE || __builtin_isfinite(lo) ? rest[2 * e] - lo : 0.0f;
+      rest[2 * e + 1] = FINITE || __builtin_isfinite(hi) ? rest[2 * e + 1] - hi : 0.0f;
     }
   }
 }
@@ -131,11 +131,10 @@ struct Request {
   int q0, nq, len, rows, off;   // first query row, query tokens, keys, rows per KV head, position of the first query
   Kv4Split split;
   __device__ __forceinline__ Request(const Kv4AttnK& a, int r) {
-    const int G = a.Hq / a.Hkv;
     q0 = min(max(a.cu[r], 0), a.total_q);
     nq = max(min(min(a.cu[r + 1], a.total_q) - q0, a.max_q), 0);
-    len = max(min(a.lens[r], (int)min((int64_t)a.max_seqlen, (int64_t)a.max_blocks * kBlock)), 0);
-    rows = nq * G;
+    len = max(min(a.lens[r], a.max_keys), 0);
+    rows = nq * a.G;
     off = len - nq;
     split = kv4_split(rows, len);
   }
@@ -170,14 +169,17 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kern
   constexpr int OP = D + 4;                   // LDS row pitch
   __shared__ __attribute__((aligned(16))) float so[NW][16][OP];
   __shared__ float sm[NW][16], sl[NW][16];
-  int idx = blockIdx.x;
-  const int h = idx % a.Hkv;
-  idx /= a.Hkv;
-  const int c = idx / tiles, tile = idx % tiles, r = blockIdx.y;   // (chunks slowest, as below)
+  // chunks slowest: workgroups beyond a request's last chunk end at once, and between live ones they would put
+  // these on a few shader engines
+  const int c = blockIdx.y;
+  uint32_t idx = blockIdx.x;
+  const int h = idx % (uint32_t)a.Hkv;
+  idx /= (uint32_t)a.Hkv;
+  const int tile = idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;
   const Request q(a, r);
   const int row0 = tile * 16 * MT;
   if (row0 >= q.rows || c >= q.split.n || (sizeof(T) == 2 && q.rows > kKv4FewRows)) return;
-  const int G = a.Hq / a.Hkv;
+  const int G = a.G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lg = lane >> 4;
@@ -209,8 +211,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kern
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       next_id[j] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + j);
-      if (next_id[j] >= 0) next[j].load(pool + next_id[j] * block_bytes, lane);
-      else next[j].clear();
+      next[j].load(pool + max(next_id[j], 0) * block_bytes, lane);   // (a missing block: any bytes, dropped below)
     }
   };
   if (steps > 0) fetch(0);
@@ -245,9 +246,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kern
     Page<D> pg[2] = {next[0], next[1]};
     const int id[2] = {next_id[0], next_id[1]};
     if (i + 1 < steps) fetch(i + 1);
-    if (kb + 32 > q.len) {
+    if (kb + 32 > q.len || id[0] < 0 || id[1] < 0) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) pg[j].drop_values_from(q.len - kb - 16 * j, lane);
+      for (int j = 0; j < 2; ++j) pg[j].drop_values_from(id[j] < 0 ? 0 : q.len - kb - 16 * j, lane);
     }
     f32x4_t sc[MT][2];
 #pragma unroll
@@ -275,27 +276,34 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kern
         for (int e = 0; e < 8; ++e)
           if (id[e >> 2] < 0 || kb + 16 * (e >> 2) + 4 * lg + (e & 3) > lim[t]) s[e] = kNegInf;
       }
-      float top = s[0];
+      // the maximum is raised only when a probability would reach 2^64 (or is not a number): the same softmax,
+      // and no maximum over the lanes in most steps
+      float p[8], psum;
+      auto expo = [&](float neg) {
+        psum = 0.0f;
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float mn = fmaxf(m[t], top * a.scale);
-      const float base = mn == kNegInf ? 0.0f : mn;
-      if (__any(mn > m[t])) {
-        const float f = __builtin_amdgcn_exp2f(m[t] - base);
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, neg));
+          psum += p[e];
+        }
+      };
+      expo(-m[t]);
+      if (__any(!(psum < 0x1p64f))) {
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mn = fmaxf(m[t], top * a.scale);
+        const float f = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
         l[t] *= f;
 #pragma unroll
         for (int u = 0; u < NU; ++u) o[t][u] *= f;
         m[t] = mn;
+        expo(mn == kNegInf ? 0.0f : -mn);
       }
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale, -base));
-        l[t] += p[e];
-      }
-      split_parts<NP>(p, pf[t]);
+      l[t] += psum;
+      split_parts<NP, true>(p, pf[t]);
     }
     // a NaN group among the values of keys that some rows see and some do not: these rows get it, the others
     // nothing
@@ -419,16 +427,15 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int t
   constexpr int NBUF = 3;
   __shared__ __attribute__((aligned(1024))) char smem[2 * NBUF * TILEB];   // [buffer][K], [buffer][V]
   __shared__ int s_nan[NBUF];         // NaN groups among the values of the buffer's tile (replaced by zero)
-  int idx = blockIdx.x;
-  const int h = idx % a.Hkv;
-  idx /= a.Hkv;
-  // chunks slowest: workgroups beyond a request's last chunk end at once, and between live ones they would put
-  // these on a few shader engines; later rows see more keys and come first
-  const int c = idx / tiles, tile = tiles - 1 - idx % tiles, r = blockIdx.y;
+  const int c = blockIdx.y;           // (slowest, as above)
+  uint32_t idx = blockIdx.x;
+  const int h = idx % (uint32_t)a.Hkv;
+  idx /= (uint32_t)a.Hkv;
+  const int tile = tiles - 1 - idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;   // later rows see more keys: first
   const Request q(a, r);
   const int row0 = tile * kWideCols;
   if (q.rows <= kKv4FewRows || row0 >= q.rows || c >= q.split.n) return;
-  const int G = a.Hq / a.Hkv;
+  const int G = a.G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hg = lane >> 5;
@@ -705,7 +712,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   const int r = blockIdx.y, h = blockIdx.x % a.Hkv;
   const Request q(a, r);
   if (q.split.n == 1) return;
-  const int G = a.Hq / a.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = q.split.n;   // n <= 64: a chunk per lane
+  const int G = a.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = q.split.n;   // n <= 64: a chunk per lane
   for (int row = blockIdx.x / a.Hkv; row < q.rows; row += gridDim.x / a.Hkv) {
     const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + row;
     const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);
@@ -754,20 +761,20 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
 template <typename T, int D>
 static hipError_t launch_kv4(const Kv4AttnK& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
-  const int splits = kv4_max_chunks(a.max_seqlen);
+  const int splits = kv4_max_chunks(a.max_keys);
   if constexpr (sizeof(T) == 2) {
     if (rows > kKv4FewRows) {
       const int wide = (int)((rows + kWideCols - 1) / kWideCols);
-      hipLaunchKernelGGL((kv4_attn_wide_kernel<D>), dim3((unsigned)(wide * splits * a.Hkv), (unsigned)a.n_req), dim3(512), 0, s, a,
+      hipLaunchKernelGGL((kv4_attn_wide_kernel<D>), dim3((unsigned)(wide * a.Hkv * a.n_req), (unsigned)splits), dim3(512), 0, s, a,
                          wide);
     }
   }
   const int64_t few = sizeof(T) == 2 && rows > kKv4FewRows ? kKv4FewRows : rows;
   if (few <= 16) {
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 1, 4>), dim3((unsigned)(splits * a.Hkv), (unsigned)a.n_req), dim3(256), 0, s, a, 1);
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 1, 4>), dim3((unsigned)(a.Hkv * a.n_req), (unsigned)splits), dim3(256), 0, s, a, 1);
   } else {
     const int tiles = (int)((few + 31) / 32);
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 4>), dim3((unsigned)(tiles * splits * a.Hkv), (unsigned)a.n_req), dim3(256), 0, s,
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 4>), dim3((unsigned)(tiles * a.Hkv * a.n_req), (unsigned)splits), dim3(256), 0, s,
                        a, tiles);
   }
   if (splits > 1) {

@@ -1,6 +1,7 @@
 // Host side of the decoding calls (include/sx_decode.h): argument validation and dispatch.
 #include "sx_decode.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "sx_kv4.h"
@@ -14,7 +15,7 @@ namespace {
 using sx::reportf;
 
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - ((int64_t)1 << 16);   // of a one-dimensional launch
-constexpr int kMaxGridY = 65535;
+constexpr int kMaxRequests = 65535;
 constexpr int kMaxSlotRequests = 65536;
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -331,13 +332,12 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   if ((st = check_pool(pool, n_blocks)) != SX_OK) return st;
   if (!cu_q || !seq_lens || (max_blocks > 0 && !block_table) || !out) return reportf(SX_EINVAL, "sx_kv4_attn: NULL argument");
   if (!aligned16(out)) return reportf(SX_EINVAL, "out is not 16-byte aligned");
-  if (n_requests > kMaxGridY) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: more than %d requests", kMaxGridY);
   const int64_t G = desc->n_q_heads / desc->n_kv_heads;
   if (max_q > total_q) max_q = total_q;
   if ((int64_t)max_q * G >= ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_q %d too large", max_q);
   if (max_seqlen > ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_seqlen above 2^30");
-  const int64_t tiles = (max_q * G + 15) / 16;
-  if (tiles * sx::kv4_max_chunks(max_seqlen) * desc->n_kv_heads * 256 >= kMaxThreads)
+  const int64_t tiles = std::max<int64_t>((max_q * G + 255) / 256, std::min<int64_t>((max_q * G + 15) / 16, esize(desc) == 4 ? INT32_MAX : 4));
+  if (n_requests > kMaxRequests || tiles * desc->n_kv_heads * n_requests * 512 >= kMaxThreads)
     return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: %d requests of %d query tokens exceed one launch", n_requests, max_q);
   int64_t part_rows;
   const int64_t need = workspace_of(desc, n_requests, max_q, max_seqlen, &part_rows);
@@ -362,9 +362,10 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   a.n_req = n_requests;
   a.total_q = total_q;
   a.max_q = max_q;
-  a.max_seqlen = max_seqlen;
+  a.max_keys = (int)std::min<int64_t>(max_seqlen, (int64_t)max_blocks * sx::kBlock);
   a.Hq = desc->n_q_heads;
   a.Hkv = desc->n_kv_heads;
+  a.G = (int)G;
   a.scale = (float)((double)sx::softmax_scale(desc) * 1.4426950408889634074);
   if (SX_DEVICE_CHECKS) {
     int v[4] = {0, 0, 0, 0};

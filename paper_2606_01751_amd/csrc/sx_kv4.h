@@ -18,23 +18,21 @@ __host__ __device__ constexpr int kv4_v_scales(int d) { return 16 * d + d / 2; }
 // length, by its own sizes alone, so that its result does not depend on the rest of the batch: at least
 // kKv4Chunk keys each, at most kKv4Splits of them, and at most kKv4PartRows partial rows in all (few rows
 // need the split to fill the chip; many rows fill it by themselves).
-constexpr int kKv4Chunk = 512;
+constexpr int kKv4Chunk = 1024;
 constexpr int kKv4Splits = 64;
 constexpr int kKv4PartRows = 4096;
 constexpr int kKv4Step = 128;    // a chunk's length is a multiple of this
 struct Kv4Split {
   int n, keys;   // chunks, and keys of each but the last
 };
-__host__ __device__ inline Kv4Split kv4_split(int rows, int len) {
-  const int r16 = rows <= 16 ? 16 : rows;
-  int cap = kKv4PartRows / r16;
-  cap = cap < 1 ? 1 : cap > kKv4Splits ? kKv4Splits : cap;
-  int n = (int)(((int64_t)len + kKv4Chunk - 1) / kKv4Chunk);
-  n = n < 1 ? 1 : n > cap ? cap : n;
-  const int64_t per = ((int64_t)len + n - 1) / n;
-  const int64_t keys = (per + kKv4Step - 1) / kKv4Step * kKv4Step;
-  const int64_t used = keys > 0 ? ((int64_t)len + keys - 1) / keys : 1;
-  return {(int)(used < 1 ? 1 : used), (int)(keys > INT32_MAX ? INT32_MAX : keys)};
+__host__ __device__ inline Kv4Split kv4_split(int rows, int len) {   // (32-bit unsigned divisions: len < 2^30 + 1)
+  const uint32_t cap = rows <= 16 ? kKv4PartRows / 16 : (uint32_t)kKv4PartRows / (uint32_t)rows;
+  const uint32_t most = cap < 1 ? 1 : cap > kKv4Splits ? kKv4Splits : cap;
+  uint32_t n = ((uint32_t)len + kKv4Chunk - 1) / kKv4Chunk;
+  n = n < 1 ? 1 : n > most ? most : n;
+  const uint32_t keys = (((uint32_t)len + n - 1) / n + kKv4Step - 1) / kKv4Step * kKv4Step;
+  const uint32_t used = keys > 0 ? ((uint32_t)len + keys - 1) / keys : 1;
+  return {(int)(used < 1 ? 1 : used), (int)keys};
 }
 // most chunks, and most partial rows (rows x chunks, where there is more than one chunk), of a request of
 // at most `rows` rows and `len` keys
@@ -111,7 +109,7 @@ struct Kv4AttnK {
   float* part;          // [n_req][Hkv][part_rows][D] unnormalised partial outputs
   float2* part_ml;      // [n_req][Hkv][part_rows] (max, sum), base-2 scores
   int64_t n_blocks, part_rows;
-  int max_blocks, n_req, total_q, max_q, max_seqlen, Hq, Hkv;
+  int max_blocks, n_req, total_q, max_q, max_keys, Hq, Hkv, G;   // max_keys: min(max_seqlen, max_blocks * 16)
   float scale;          // softmax scale * log2(e)
 };
 hipError_t launch_kv4_attn(const Kv4AttnK& a, int D, bool f32, hipStream_t s);
