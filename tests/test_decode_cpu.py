@@ -82,9 +82,9 @@ def test_kv4_sizes():
     assert sx.lib().sx_kv4_record_bytes(ctypes.byref(desc(head_dim=80)), ctypes.byref(n)) == sx.SX_EUNSUPPORTED
     assert sx.lib().sx_kv4_record_bytes(ctypes.byref(desc()), None) == sx.SX_EINVAL
     # no split, no workspace; it grows with every bound
-    assert sx.kv4_attn_workspace(desc(), 8, 1, 512) == 0
+    assert sx.kv4_attn_workspace(desc(), 8, 1, 256) == 0
     last = 0
-    for q, s in ((1, 513), (1, 4096), (4, 4096), (64, 4096), (64, 131072)):
+    for q, s in ((1, 512), (1, 8192), (4, 8192), (64, 8192), (64, 131072)):
         w = sx.kv4_attn_workspace(desc(), 8, q, s)
         assert w >= last and w % 8 == 0
         last = w
@@ -131,8 +131,8 @@ def test_kv4_blocks_refusals(name):
 
 
 def attn_args(**kw):
-    a = dict(q=A, qld=1024, cu=A + 0x10000, lens=A + 0x11000, table=A + 0x12000, width=64, nr=2, tq=2, mq=1, ms=1024,
-             pool=A + 0x20000, nb=64, out=A + 0x30000, lse=None, ws=A + 0x40000, wb=1 << 24)
+    a = dict(q=A, qld=1024, cu=A + 0x10000, lens=A + 0x11000, table=A + 0x12000, width=64, nr=2, tq=2, mq=1, ms=131072,
+             pool=A + 0x20000, nb=64, out=A + 0x30000, lse=None, ws=A + 0x40000, wb=1 << 28)
     a.update(kw)
     return [a[k] for k in ("q", "qld", "cu", "lens", "table", "width", "nr", "tq", "mq", "ms", "pool", "nb", "out", "lse",
                            "ws", "wb")] + [None]
