@@ -161,7 +161,7 @@ __device__ __forceinline__ void for_each(F&& f) {
 // once.  Writes the rows' results, or their parts where the request's keys are split.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 4 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
   constexpr int NC = D / 32;                  // 32-element pieces of a row
   constexpr int NU = D / 16;                  // 16-column tiles of V
   constexpr int NQ = sizeof(T) == 4 ? 3 : 1;  // bfloat16 parts of a query element, and of a probability
@@ -702,24 +702,30 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int t
   }
 }
 
-// The parts of split requests: one workgroup per row, its four waves the chunks w, w + 4, ... in turn (their
-// loads all in flight at once), then the waves in order.
+// The parts of split requests.  A wave takes the chunks w, w + W, ... of a row (their loads all in flight at
+// once): W = 1 and four rows a workgroup for up to 16 chunks, else W = 4 waves a row, added in order.  One row
+// a workgroup for any number of chunks took 8.4 us where 1792 rows had 5 chunks each.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   constexpr int E = D / 64;                  // elements per lane
   constexpr int PER = kKv4Splits / 4;        // most chunks per wave
   __shared__ float so[4][D];
-  const int r = blockIdx.y, h = blockIdx.x % a.Hkv;
+  const int r = blockIdx.y, h = blockIdx.x % (uint32_t)a.Hkv;
   const Request q(a, r);
   if (q.split.n == 1) return;
-  const int G = a.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = q.split.n;   // n <= 64: a chunk per lane
-  for (int row = blockIdx.x / a.Hkv; row < q.rows; row += gridDim.x / a.Hkv) {
+  const int G = a.G, lane = threadIdx.x & 63, n = q.split.n;   // n <= 64: a chunk per lane
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool alone = n <= PER;               // one wave a row
+  const int first = blockIdx.x / (uint32_t)a.Hkv, step = gridDim.x / (uint32_t)a.Hkv;
+  for (int base_row = alone ? first * 4 : first; base_row < q.rows; base_row += alone ? step * 4 : step) {
+    const int row = min(alone ? base_row + wave : base_row, q.rows - 1);
+    const int c0 = alone ? 0 : wave, cs = alone ? 1 : 4;
     const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + row;
     const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);
     float x[PER][E];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = 4 * i + wave;
+      const int c = c0 + cs * i;
       const float* src = a.part + (at + (int64_t)c * q.rows) * D + lane * E;
 #pragma unroll
       for (int e = 0; e < E; ++e) x[i][e] = c < n ? src[e] : 0.0f;
@@ -735,24 +741,33 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
     for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const float fc = __shfl(f, 4 * i + wave, 64);
+      const int c = c0 + cs * i;
+      const float fc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), c & 63));
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x[i][e], 4 * i + wave < n ? fc : 0.0f, acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x[i][e], c < n ? fc : 0.0f, acc[e]);
     }
+    if (!alone) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) so[wave][lane * E + e] = acc[e];
-    __syncthreads();
-    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-    const int64_t to = (int64_t)(q.q0 + row / G) * a.Hq + h * G + row % G;
-    if (threadIdx.x < D / 2) {
-      const int d = threadIdx.x * 2;
-      const float u = (so[0][d] + so[1][d]) + (so[2][d] + so[3][d]), v = (so[0][d + 1] + so[1][d + 1]) + (so[2][d + 1] + so[3][d + 1]);
-      T* dst = (T*)a.out + to * D + d;
-      if constexpr (sizeof(T) == 2) *(uint32_t*)dst = pack_bf16x2(u * inv, v * inv);
-      else *(float2*)dst = make_float2(u * inv, v * inv);
+      for (int e = 0; e < E; ++e) so[wave][lane * E + e] = acc[e];
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        acc[e] = (so[0][lane * E + e] + so[1][lane * E + e]) + (so[2][lane * E + e] + so[3][lane * E + e]);
+      __syncthreads();
     }
-    if (a.lse && threadIdx.x == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
-    __syncthreads();
+    if (alone ? base_row + wave < q.rows : wave == 0) {
+      const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+      const int64_t to = (int64_t)(q.q0 + row / G) * a.Hq + h * G + row % G;
+      T* dst = (T*)a.out + to * D + lane * E;
+      if constexpr (E == 1) {
+        if constexpr (sizeof(T) == 2) *dst = (uint16_t)pack_bf16x2(acc[0] * inv, 0.0f);
+        else *dst = acc[0] * inv;
+      } else {
+        if constexpr (sizeof(T) == 2) *(uint32_t*)dst = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+        else *(float2*)dst = make_float2(acc[0] * inv, acc[1] * inv);
+      }
+      if (a.lse && lane == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
+    }
   }
 }
 

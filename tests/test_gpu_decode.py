@@ -407,6 +407,30 @@ def test_kv4_attn_no_dependence_on_the_batch_or_the_bounds():
         assert torch.equal(o, out[b.cu[r]:b.cu[r + 1]]), r
 
 
+def test_kv4_attn_any_workspace_and_many_calls_on_one():
+    # the same bits whatever the workspace held, call after call of different sizes
+    small = Batch([(1, 9000), (1, 70), (1, 40000), (3, 2500)], 8, 2, 128, "bf16", seed=9)
+    large = Batch([(12, 30000), (1, 5000)], 16, 2, 64, "f32", seed=10)
+    many = Batch([(1, 40000), (1, 20000)], 64, 1, 64, "bf16", seed=11)
+    size = max(sx.kv4_attn_workspace(b.desc, len(b.nq), max(b.nq), max(b.nk)) for b in (small, large, many))
+    want = [b.run() for b in (small, large, many)]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for i in range(30):
+        if i % 5 == 0:
+            ws = torch.randint(0, 256, (size,), generator=g, dtype=torch.uint8, device="cuda") if i else \
+                torch.zeros(size, dtype=torch.uint8, device="cuda")
+        for b, (o, l) in zip((small, large, many), want):
+            out, lse = b.run(workspace=ws)
+            assert torch.equal(out, o) and torch.equal(lse, l), i
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,nq,nk", [(64, 1, 64, "bf16", 1, 18000), (8, 1, 64, "f32", 30, 9000), (4, 1, 128, "bf16", 16, 17500),
+                                                  (4, 1, 64, "bf16", 64, 6000)])
+def test_kv4_attn_split_rows(hq, hkv, d, dtype, nq, nk):
+    # 17 and more chunks, of few and of many rows
+    Batch([(nq, nk), (1, nk // 2)], hq, hkv, d, dtype, seed=nk).check()
+
+
 def test_kv4_attn_lengths_beyond_the_bounds_are_cut():
     # the release library never reads past what the host was told: 2 blocks a row, 20 keys, 3 queries
     b = Batch([(1, 32), (1, 32)], 4, 2, 64, "bf16", seed=3)
