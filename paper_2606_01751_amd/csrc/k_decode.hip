@@ -16,7 +16,7 @@ namespace {
 // own range of token indices from the run in LDS; workgroup 0 writes what there is one of per request.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSlotRun = 256;    // requests a run, and threads
-constexpr int kSlotTokens = 4;   // tokens per thread and workgroup at the least
+constexpr int kSlotTokens = 1;   // tokens per thread (300 requests, 131072 tokens: 6.4 us; 7.2 with 2, 7.9 with 4)
 
 struct SlotRun {
   int64_t tok0, blk0;             // prefix sums before the run
@@ -35,6 +35,12 @@ __device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {   // inclusi
   return v;
 }
 
+// ceil(n / b)
+__device__ __forceinline__ int64_t blocks_of(uint32_t n, uint32_t b) {
+  const uint32_t q = n / b;
+  return (int64_t)q + (q * b != n);
+}
+
 __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, int per_wg) {
   __shared__ SlotRun run;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -42,15 +48,15 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
   const int64_t t0 = (int64_t)(blockIdx.x - 1) * per_wg;   // this workgroup's token indices (not workgroup 0)
   const int64_t t1 = min(t0 + per_wg, (int64_t)a.max_tokens);
   const int64_t head = a.free_head ? max(a.free_head[0], 0) : 0;
-  const int b = a.block;
+  const uint32_t b = a.block;
   int64_t tok = 0, blk = 0, missing = 0;
   for (int r0 = 0; r0 < a.n_req; r0 += kSlotRun) {
     const int r = r0 + tid;
     const int ctx = r < a.n_req ? max(a.ctx[r], 0) : 0;
     const int add = r < a.n_req ? (a.add ? max(a.add[r], 0) : 1) : 0;
-    const int64_t len = (int64_t)ctx + add;
-    const int64_t have = ((int64_t)ctx + b - 1) / b;
-    const int64_t need = max(min((len + b - 1) / b, (int64_t)a.max_blocks) - have, (int64_t)0);
+    const int64_t len = (int64_t)ctx + add;   // (below 2^32)
+    const int64_t have = blocks_of((uint32_t)ctx, b);
+    const int64_t need = max(min(blocks_of((uint32_t)len, b), (int64_t)a.max_blocks) - have, (int64_t)0);
     int64_t st = wave_scan(add, lane), sb = wave_scan(need, lane);
     if (lane == 63) {
       run.wave_tok[wave] = st;
@@ -93,8 +99,9 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
 #pragma unroll
         for (int o = kSlotRun / 2; o >= 1; o >>= 1)
           if (run.tok[lo + o] <= x) lo += o;
-        const int64_t p = (int64_t)run.ctx[lo] + (x - run.tok[lo]);
-        const int64_t bi = p / b, hv = ((int64_t)run.ctx[lo] + b - 1) / b;
+        const uint32_t p = (uint32_t)run.ctx[lo] + (uint32_t)(x - run.tok[lo]);   // (below 2^32)
+        const int64_t bi = p / b, hv = blocks_of((uint32_t)run.ctx[lo], b);
+        const uint32_t off = p - (uint32_t)bi * b;
         int32_t* row = a.table + (int64_t)(r0 + lo) * a.max_blocks;
         int id = -1;
         if (bi < a.max_blocks) {
@@ -103,11 +110,11 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
           } else {
             const int64_t f = head + blk + run.blk[lo] + bi - hv;
             if (f >= 0 && f < a.n_free) id = a.free_blocks[f];
-            if (p % b == 0) row[bi] = id;
+            if (off == 0) row[bi] = id;
           }
         }
-        const int64_t slot = (int64_t)id * b + p % b;
-        a.pos[i] = (int)min(p, (int64_t)INT32_MAX);
+        const int64_t slot = (int64_t)id * b + off;
+        a.pos[i] = (int)min(p, (uint32_t)INT32_MAX);
         a.slots[i] = id >= 0 && slot <= INT32_MAX ? (int)slot : -1;
       }
     }
@@ -137,60 +144,106 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
 // (y1, y2) with frequency theta_p goes to (y1 c - y2 s, y2 c + y1 s), c, s = cos, sin(pos theta_p) formed in
 // float64 once per (token, pair) and shared by the token's heads through LDS.  D / 8 lanes hold a head, 8
 // elements each; with NEOX pairs a lane's partner elements sit D / 16 lanes away.
+// A workgroup takes 256 / (D / 2) tokens and, of their heads, one of `parts` shares: few tokens are bound by latency
+// (the first share of the rows is loaded before the angles are formed), many by HBM.
 // ---------------------------------------------------------------------------------------------
+
+// cos and sin of phi >= 0, rounded to float32.  phi = n pi/2 + r with |r| <= pi/4, pi/2 in two float64 parts (the first
+// is off by 2^-54, the second makes up for n times that; positions below 2^31 keep n below 2^31 for bases of 1 and more);
+// the Taylor polynomials of r up to r^13 and r^14 are off by less than 2^-45, far below half a unit of float32.
+__device__ __forceinline__ void cos_sin(double phi, float* c, float* s) {
+  const double n = __builtin_rint(phi * 0.63661977236758134308);
+  double r = __builtin_fma(n, -1.57079632679489655800, phi);
+  r = __builtin_fma(n, -6.12323399573676603587e-17, r);
+  const double z = r * r;
+  double ps = 1.0 / 6227020800.0, pc = -1.0 / 87178291200.0;
+  ps = __builtin_fma(ps, z, -1.0 / 39916800.0);
+  pc = __builtin_fma(pc, z, 1.0 / 479001600.0);
+  ps = __builtin_fma(ps, z, 1.0 / 362880.0);
+  pc = __builtin_fma(pc, z, -1.0 / 3628800.0);
+  ps = __builtin_fma(ps, z, -1.0 / 5040.0);
+  pc = __builtin_fma(pc, z, 1.0 / 40320.0);
+  ps = __builtin_fma(ps, z, 1.0 / 120.0);
+  pc = __builtin_fma(pc, z, -1.0 / 720.0);
+  ps = __builtin_fma(ps, z, -1.0 / 6.0);
+  pc = __builtin_fma(pc, z, 1.0 / 24.0);
+  pc = __builtin_fma(pc, z, -0.5);
+  const float fs = (float)__builtin_fma(ps * z, r, r), fc = (float)__builtin_fma(pc, z, 1.0);
+  const int q = (int)__builtin_fma(-4.0, __builtin_floor(n * 0.25), n);   // quadrant
+  const float a = q & 1 ? fs : fc, b = q & 1 ? fc : fs;
+  *c = (q + 1) & 2 ? -a : a;
+  *s = q & 2 ? -b : b;
+}
+
 template <typename T, int D, bool NEOX, bool ROWS>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRopeK a) {
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRopeK a, int parts) {
   constexpr int TB = 256 / (D / 2);   // tokens per workgroup
   constexpr int LPH = D / 8;          // lanes per head
+  constexpr int HPW = 256 / LPH;      // heads a pass of the workgroup
   __shared__ __attribute__((aligned(16))) float cs[TB][D / 2], sn[TB][D / 2];
-  __shared__ int64_t trow[TB];        // token row, -1: none
-  const int n0 = blockIdx.x * TB;
-  const int tb0 = threadIdx.x / (D / 2), pr = threadIdx.x % (D / 2);
-  {
+  __shared__ int64_t rows[TB];        // token rows, -1: none
+  const int part = blockIdx.x % (uint32_t)parts, n0 = blockIdx.x / (uint32_t)parts * TB;
+  const int live = ROWS ? min(a.n_rows[blockIdx.y], a.max_rows) : a.n;   // rows of the call
+  if (ROWS && n0 >= live) return;
+  auto token = [&](int tb, int* pos) {   // token row of the workgroup's tb-th row, -1: none
     int64_t t = -1;
-    int p = -1;
-    if constexpr (ROWS) {
-      const ReqDev rq = a.reqs[blockIdx.y];
-      if (n0 >= min(a.n_rows[blockIdx.y], a.max_rows)) return;
-      if (n0 + tb0 < min(a.n_rows[blockIdx.y], a.max_rows)) {
-        t = (int64_t)rq.tok_off + a.rows[rq.tok_off + n0 + tb0];
-        p = a.tok_pos[t];
+    if (n0 + tb < live) {
+      if constexpr (ROWS) {
+        const ReqDev rq = a.reqs[blockIdx.y];
+        t = (int64_t)rq.tok_off + a.rows[rq.tok_off + n0 + tb];
+        *pos = a.tok_pos[t];
+      } else {
+        t = n0 + tb;
+        *pos = a.pos[t];
       }
-    } else if (n0 + tb0 < a.n) {
-      t = n0 + tb0;
-      p = a.pos[t];
+      if (*pos < 0) t = -1;
     }
-    if (p < 0) t = -1;
-    const double phi = (double)max(p, 0) * (ROWS ? a.d_theta[pr] : a.theta[pr]);
-    cs[tb0][pr] = (float)cos(phi);
-    sn[tb0][pr] = (float)sin(phi);
-    if (pr == 0) trow[tb0] = t;
-  }
-  __syncthreads();
+    return t;
+  };
   const int H = a.Hq + a.Hkv;
   const int hl = threadIdx.x % LPH;   // lane of its head
-  for (int x = threadIdx.x / LPH; x < TB * H; x += 256 / LPH) {
-    const int tb = x / H, h = x - tb * H;
-    const int64_t t = trow[tb];
-    const bool isq = h < a.Hq;
-    const bool live = t >= 0;
-    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (live) {
-      const T* src = isq ? (const T*)a.q + t * a.q_ld + h * D : (const T*)a.k + t * a.k_ld + (h - a.Hq) * D;
-      load8(src + hl * 8, y);
+  const int items = TB * H, per = (items + parts * HPW - 1) / (parts * HPW) * HPW;   // (token, head) items of a share
+  const int x0 = part * per + threadIdx.x / LPH, x1 = min(part * per + per, items);
+  int64_t t = -1;
+  int h = 0, tb = 0;
+  float y[8];
+  auto fetch = [&](int x, auto row_of) {
+    tb = x / (uint32_t)H;
+    h = x - tb * H;
+    t = x < x1 ? row_of(tb) : -1;
+    if (t >= 0) {
+      load8((h < a.Hq ? (const T*)a.q + t * a.q_ld + h * D : (const T*)a.k + t * a.k_ld + (h - a.Hq) * D) + hl * 8, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = 0.0f;
     }
-    const void* gamma = isq ? a.gq : a.gk;
-    if (gamma) {
+  };
+  fetch(x0, [&](int i) {
+    int pos;
+    return token(i, &pos);
+  });
+  float gq[8], gk[8];
+  if (a.gq) load8((const T*)a.gq + hl * 8, gq);
+  if (a.gk) load8((const T*)a.gk + hl * 8, gk);
+  {
+    const int pr = threadIdx.x % (D / 2), mine = threadIdx.x / (D / 2);
+    int pos = 0;
+    const int64_t row = token(mine, &pos);
+    if (pr == 0) rows[mine] = row;
+    cos_sin((double)max(pos, 0) * (ROWS ? a.d_theta[pr] : a.theta[pr]), &cs[mine][pr], &sn[mine][pr]);
+  }
+  __syncthreads();
+  for (int x = x0; x < x1; x += HPW) {
+    const bool isq = h < a.Hq;
+    if (isq ? a.gq != nullptr : a.gk != nullptr) {
       float ss = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
 #pragma unroll
       for (int o = LPH / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o, 64);
       const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-      float g[8];
-      load8((const T*)gamma + hl * 8, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * g[e];
+      for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * (isq ? gq[e] : gk[e]);
     }
     float o8[8];
     if constexpr (NEOX) {
@@ -210,10 +263,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRopeK a) {
         o8[2 * e + 1] = y[2 * e + 1] * c + y[2 * e] * s;
       }
     }
-    if (live) {
-      T* dst = isq ? (T*)a.qo + t * a.qo_ld + h * D : (T*)a.ko + t * a.ko_ld + (h - a.Hq) * D;
-      store8(dst + hl * 8, o8);
-    }
+    T* dst = isq ? (T*)a.qo + t * a.qo_ld + h * D : (T*)a.ko + t * a.ko_ld + (h - a.Hq) * D;
+    const bool put = t >= 0;
+    if (put) store8(dst + hl * 8, o8);
+    if (x + HPW < x1) fetch(x + HPW, [&](int i) { return rows[i]; });
   }
 }
 
@@ -229,12 +282,20 @@ hipError_t launch_append_slots(const AppendSlotsK& a, hipStream_t s) {
 
 template <typename T, int D, bool NEOX>
 static void launch_qk(const QkNormRopeK& a, hipStream_t s) {
-  constexpr int TB = 256 / (D / 2);
+  constexpr int TB = 256 / (D / 2), HPW = 256 / (D / 8);
+  const int rows = a.rows ? a.max_rows : a.n;
+  const int64_t groups = (int64_t)((rows + TB - 1) / TB) * (a.rows ? a.n_req : 1);
+  // shares of a group's heads: up to 2048 workgroups, one pass of the workgroup each at the least.  256 tokens of 32 / 8
+  // heads (d = 128): 4.9 us in ten shares, 11.4 in one.
+  const int passes = (TB * (a.Hq + a.Hkv) + HPW - 1) / HPW;
+  const int64_t want = groups > 0 ? 2048 / groups : 1;
+  const int parts = (int)(want < 1 ? 1 : want > passes ? passes : want);
   if (a.rows)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, D, NEOX, true>), dim3((unsigned)((a.max_rows + TB - 1) / TB), (unsigned)a.n_req),
-                       dim3(256), 0, s, a);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, D, NEOX, true>), dim3((unsigned)((rows + TB - 1) / TB * parts), (unsigned)a.n_req),
+                       dim3(256), 0, s, a, parts);
   else
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, D, NEOX, false>), dim3((unsigned)((a.n + TB - 1) / TB)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, D, NEOX, false>), dim3((unsigned)((rows + TB - 1) / TB * parts)), dim3(256), 0, s,
+                       a, parts);
 }
 
 hipError_t launch_qk_norm_rope(const QkNormRopeK& a, int D, bool f32, bool neox, hipStream_t s) {

@@ -158,10 +158,14 @@ __device__ __forceinline__ void for_each(F&& f) {
 // ---------------------------------------------------------------------------------------------
 // Few query rows: one workgroup takes 16 MT rows of one KV head over one chunk of keys, its NW waves steps of
 // two blocks in turn; the next step's codes are loaded while a step is computed, the block ids of 32 steps at
-// once.  Writes the rows' results, or their parts where the request's keys are split.
+// once.  Writes the rows' results, or their parts where the request's keys are split.  (Adding them up in the
+// workgroup that ends last saved nothing over the merge launch: 38.6 us for 34.6, 50.2 for 47.5 on the two cases
+// below.)  Bound by HBM where there is work for every compute unit: 64 requests of up to 8192 keys (28 / 4 heads, d =
+// 128) 47.5 us with the merge, 3.4 TB/s; 256 of 1024 keys (32 / 8) 58.8 us, 4.9 TB/s; one of 131072 keys 34.6 us, 4.1
+// TB/s; a plain streaming read reaches 5.5 - 6.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 4 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
   constexpr int NC = D / 32;                  // 32-element pieces of a row
   constexpr int NU = D / 16;                  // 16-column tiles of V
   constexpr int NQ = sizeof(T) == 4 ? 3 : 1;  // bfloat16 parts of a query element, and of a probability
@@ -204,17 +208,19 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 4 : 2) : 1) vo
     return id < a.n_blocks ? id : -1;
   };
   int ids = load_ids(0);
-  Page<D> next[2];
-  int next_id[2];
-  auto fetch = [&](int i) {
+  // codes of the current and the next step: the loop below names the slots in turn, since a register copy would
+  // wait for its load.  (Two and three steps ahead were no faster: 36 us and 37.5 for one token over 131072 keys.)
+  Page<D> page[2][2];
+  int page_id[2][2];
+  auto fetch = [&](int i, Page<D> (&pg)[2], int (&id)[2]) __attribute__((always_inline)) {
     if (i > 0 && (i & 31) == 0) ids = load_ids(i >> 5);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      next_id[j] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + j);
-      next[j].load(pool + max(next_id[j], 0) * block_bytes, lane);   // (a missing block: any bytes, dropped below)
+      id[j] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + j);
+      pg[j].load(pool + max(id[j], 0) * block_bytes, lane);   // (a missing block: any bytes, dropped below)
     }
   };
-  if (steps > 0) fetch(0);
+  if (steps > 0) fetch(0, page[0], page_id[0]);
 
   bf16x8_t qf[MT][NC][NQ];
 #pragma unroll
@@ -241,11 +247,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 4 : 2) : 1) vo
     for (int u = 0; u < NU; ++u) o[t][u] = (f32x4_t){0, 0, 0, 0};
   }
 
-  for (int i = 0; i < steps; ++i) {
+  auto step = [&](int i, Page<D> (&pg)[2], const int (&id)[2], Page<D> (&next)[2], int (&next_id)[2]) __attribute__((always_inline)) {
     const int kb = k0 + 32 * (wave + NW * i);
-    Page<D> pg[2] = {next[0], next[1]};
-    const int id[2] = {next_id[0], next_id[1]};
-    if (i + 1 < steps) fetch(i + 1);
+    if (i + 1 < steps) fetch(i + 1, next, next_id);
     if (kb + 32 > q.len || id[0] < 0 || id[1] < 0) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) pg[j].drop_values_from(id[j] < 0 ? 0 : q.len - kb - 16 * j, lane);
@@ -338,6 +342,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 4 : 2) : 1) vo
           for (int n = NP - 1; n >= 0; --n) o[t][u] = mfma16(vf, pf[t][n], o[t][u]);
       });
     });
+  };
+  for (int i = 0; i < steps; i += 2) {
+    step(i, page[0], page_id[0], page[1], page_id[1]);
+    if (i + 1 < steps) step(i + 1, page[1], page_id[1], page[0], page_id[0]);
   }
 
 #pragma unroll
