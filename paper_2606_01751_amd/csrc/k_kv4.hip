@@ -3,9 +3,11 @@
 //   kv4_write_kernel   rows by slot, or whole blocks, rounded to 4 bits
 //   kv4_read_kernel    the same way back, exactly
 //
-// A wave takes 16 tokens of one KV head: lane l has token l / 4 and, in step `it`, the 8 elements from
-// d = 32 it + 8 (l % 4), so four neighbouring lanes hold the 32 elements that share a scale.  The scale
-// comes from the largest absolute value's bits: 2^E with 1.m >= 1.75 (m > 0x600000) needs e = E - 1, else
+// A wave takes 16 tokens of one KV head, 512 elements an instruction: lane l has 8 elements, d = 8 (l % (D / 8)), of
+// token NI (l / (D / 8)) + i in step i of NI, so an instruction moves whole rows, four neighbouring lanes hold the 32
+// elements that share a scale, and a lane's steps are neighbours in V's byte order (with D = 128 its four tokens' codes
+// are 16 consecutive bytes of a block; K's become so by a transposition over the four lanes of a group).  The
+// scale comes from the largest absolute value's bits: 2^E with 1.m >= 1.75 (m > 0x600000) needs e = E - 1, else
 // E - 2 (7 * 2^e = 1.75 * 2^(e + 2)).  The conversion instruction rounds to nearest with ties to even and
 // saturates, which is the definition; every 4-bit value is a bfloat16 value, so reading is exact.
 #include "sx_kv4_device.h"
@@ -24,14 +26,36 @@ __device__ __forceinline__ int v_code_off(int t, int d) {
   return kv4_v_codes(D) + ((t / 4 * 16 + d / (D / 16)) * 4 + t % 4) * (D / 32);
 }
 
+// Value of lane l ^ X of the same four lanes.
+template <int X>
+__device__ __forceinline__ uint32_t quad_xor(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, X == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);   // quad_perm 1032, 2301
+}
+
+// Transposes x[4] over four lanes: lane m's x[j] becomes lane j's x[m].
+__device__ __forceinline__ void quad_transpose(uint32_t (&x)[4], int m) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {
+    const uint32_t y = quad_xor<1>(m & 1 ? x[j] : x[j + 1]);
+    if (m & 1) x[j] = y;
+    else x[j + 1] = y;
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t y = quad_xor<2>(m & 2 ? x[j] : x[j + 2]);
+    if (m & 2) x[j] = y;
+    else x[j + 2] = y;
+  }
+}
+
 // Eight elements -> codes and their group's scale byte.
 __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t* byte) {
   // as integers: the absolute values order like their bits, and NaN and infinity come out on top
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+  top = max(top, quad_xor<1>(top));
+  top = max(top, quad_xor<2>(top));
   if (top >= 0x7f800000u) {
     *byte = 255;
     return 0;
@@ -73,69 +97,135 @@ __device__ __forceinline__ bool locate(const Kv4MoveK& a, int tile, int t, int h
 
 template <typename T, int D, bool BLOCKS>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4MoveK a, int tiles) {
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= (int64_t)tiles * a.Hkv) return;
-  const int tile = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
-  const int lane = threadIdx.x & 63, t = lane >> 2, m = lane & 3;
-  int64_t ko = 0, vo = 0;
-  uint8_t* rec = nullptr;
-  int tt = 0;
-  const bool live = locate<D, BLOCKS>(a, tile, t, h, &ko, &vo, &rec, &tt);
-  if (!live) return;   // (a token's four lanes leave together)
+  constexpr int LPR = D / 8, NI = LPR / 4;   // lanes a row, steps
+  const uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (item >= (uint32_t)tiles * a.Hkv) return;
+  const int tile = item / (uint32_t)a.Hkv, h = item % (uint32_t)a.Hkv;
+  const int lane = threadIdx.x & 63, d = lane % LPR * 8, m = lane & 3;
+  float k[NI][8], v[NI][8];
+  uint8_t* rec[NI];
+  int tt[NI];
+  bool live[NI];
 #pragma unroll
-  for (int it = 0; it < D / 32; ++it) {
-    const int d = it * 32 + m * 8;
-    float x[8];
-    uint32_t byte;
-    load8((const T*)a.k + ko + d, x);
-    *(uint32_t*)(rec + k_code_off<D>(tt, d)) = quantise8(x, &byte);
-    if (m == 0) rec[kv4_k_scales(D) + it * 16 + tt] = (uint8_t)byte;
-    load8((const T*)a.v + vo + d, x);
-    const uint32_t w = quantise8(x, &byte);
-    if constexpr (D == 128) {
-      *(uint32_t*)(rec + v_code_off<D>(tt, d)) = w;
-    } else {
-      *(uint16_t*)(rec + v_code_off<D>(tt, d)) = (uint16_t)w;
-      *(uint16_t*)(rec + v_code_off<D>(tt, d + 4)) = (uint16_t)(w >> 16);
+  for (int i = 0; i < NI; ++i) {
+    int64_t ko = 0, vo = 0;
+    rec[i] = nullptr;
+    tt[i] = 0;
+    if constexpr (!BLOCKS) {                 // (the rows are on their way beside the slots)
+      const int64_t row = min(tile * kBlock + lane / LPR * NI + i, a.n - 1);
+      load8((const T*)a.k + row * a.k_ld + h * D + d, k[i]);
+      load8((const T*)a.v + row * a.v_ld + h * D + d, v[i]);
     }
-    if (m == 0) rec[kv4_v_scales(D) + it * 16 + tt] = (uint8_t)byte;
+    live[i] = locate<D, BLOCKS>(a, tile, lane / LPR * NI + i, h, &ko, &vo, &rec[i], &tt[i]);
+    if (BLOCKS && live[i]) {
+      load8((const T*)a.k + ko + d, k[i]);
+      load8((const T*)a.v + vo + d, v[i]);
+    }
+  }
+  if (BLOCKS && !live[0]) return;            // (one block: all or none)
+  uint32_t kw[NI] = {}, vw[NI] = {}, kb[NI] = {}, vb[NI] = {};
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    if (live[i]) {                           // (a token's lanes stay together)
+      kw[i] = quantise8(k[i], &kb[i]);
+      vw[i] = quantise8(v[i], &vb[i]);
+    }
+  const int g = d / kKv4Group;
+  if constexpr (D == 128) {
+    // lane m of a group takes token 4 (l / 16) + m: the 16 bytes of its K, and its scales
+    uint32_t mk[4] = {kb[0], kb[1], kb[2], kb[3]}, mv[4] = {vb[0], vb[1], vb[2], vb[3]};
+    quad_transpose(kw, m);
+    const uint32_t ks = m & 2 ? (m & 1 ? mk[3] : mk[2]) : (m & 1 ? mk[1] : mk[0]);
+    const uint32_t vs = m & 2 ? (m & 1 ? mv[3] : mv[2]) : (m & 1 ? mv[1] : mv[0]);
+    uint8_t* r = rec[0];
+    int t = tt[0];
+    bool on = live[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (m == i) {
+        r = rec[i];
+        t = tt[i];
+        on = live[i];
+      }
+    if (on) {
+      *(uint4*)(r + k_code_off<D>(t, g * kKv4Group)) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
+      r[kv4_k_scales(D) + g * 16 + t] = (uint8_t)ks;
+      r[kv4_v_scales(D) + g * 16 + t] = (uint8_t)vs;
+    }
+    if constexpr (BLOCKS) {
+      *(uint4*)(rec[0] + v_code_off<D>(tt[0], d)) = make_uint4(vw[0], vw[1], vw[2], vw[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (live[i]) *(uint32_t*)(rec[i] + v_code_off<D>(tt[i], d)) = vw[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (live[i]) {
+        *(uint32_t*)(rec[i] + k_code_off<D>(tt[i], d)) = kw[i];
+        if (m == 0) {
+          rec[i][kv4_k_scales(D) + g * 16 + tt[i]] = (uint8_t)kb[i];
+          rec[i][kv4_v_scales(D) + g * 16 + tt[i]] = (uint8_t)vb[i];
+        }
+        if constexpr (!BLOCKS) {
+          *(uint16_t*)(rec[i] + v_code_off<D>(tt[i], d)) = (uint16_t)vw[i];
+          *(uint16_t*)(rec[i] + v_code_off<D>(tt[i], d + 4)) = (uint16_t)(vw[i] >> 16);
+        }
+      }
+    if constexpr (BLOCKS) {                  // tokens t, t + 1 of both column groups
+      *(uint32_t*)(rec[0] + v_code_off<D>(tt[0], d)) = __builtin_amdgcn_perm(vw[1], vw[0], 0x05040100u);
+      *(uint32_t*)(rec[0] + v_code_off<D>(tt[0], d + 4)) = __builtin_amdgcn_perm(vw[1], vw[0], 0x07060302u);
+    }
   }
 }
 
+// Streaming stores: what leaves is read by a later launch at the earliest.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 template <typename T>
 __device__ __forceinline__ void put8(T* p, uint32_t w, float s) {
-  const uint32_t u[4] = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
+  const u32x4_t u = {kv4_pair<0>(w, s), kv4_pair<1>(w, s), kv4_pair<2>(w, s), kv4_pair<3>(w, s)};
   if constexpr (sizeof(T) == 2) {
-    *(uint4*)p = make_uint4(u[0], u[1], u[2], u[3]);
+    __builtin_nontemporal_store(u, (u32x4_t*)p);
   } else {
-    const float x[8] = {bf16_lo(u[0]), bf16_hi(u[0]), bf16_lo(u[1]), bf16_hi(u[1]),
-                        bf16_lo(u[2]), bf16_hi(u[2]), bf16_lo(u[3]), bf16_hi(u[3])};
-    store8(p, x);
+    const u32x4_t a = {u[0] << 16, u[0] & 0xffff0000u, u[1] << 16, u[1] & 0xffff0000u};
+    const u32x4_t b = {u[2] << 16, u[2] & 0xffff0000u, u[3] << 16, u[3] & 0xffff0000u};
+    __builtin_nontemporal_store(a, (u32x4_t*)p);
+    __builtin_nontemporal_store(b, (u32x4_t*)p + 1);
   }
 }
 
 template <typename T, int D, bool BLOCKS>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4MoveK a, int tiles) {
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= (int64_t)tiles * a.Hkv) return;
-  const int tile = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
-  const int lane = threadIdx.x & 63, t = lane >> 2, m = lane & 3;
-  int64_t ko = 0, vo = 0;
-  uint8_t* rec = nullptr;
-  int tt = 0;
-  if (!locate<D, BLOCKS>(a, tile, t, h, &ko, &vo, &rec, &tt)) return;
+  constexpr int LPR = D / 8, NI = LPR / 4;
+  const uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (item >= (uint32_t)tiles * a.Hkv) return;
+  const int tile = item / (uint32_t)a.Hkv, h = item % (uint32_t)a.Hkv;
+  const int lane = threadIdx.x & 63, d = lane % LPR * 8;
+  int64_t ko[NI], vo[NI];
+  uint32_t kw[NI], vw[NI], ks[NI], vs[NI];
+  bool live[NI];
 #pragma unroll
-  for (int it = 0; it < D / 32; ++it) {
-    const int d = it * 32 + m * 8;
-    put8((T*)a.k + ko + d, *(const uint32_t*)(rec + k_code_off<D>(tt, d)),
-         kv4_scale(rec[kv4_k_scales(D) + it * 16 + tt]));
-    uint32_t w;
-    if constexpr (D == 128)
-      w = *(const uint32_t*)(rec + v_code_off<D>(tt, d));
-    else
-      w = *(const uint16_t*)(rec + v_code_off<D>(tt, d)) | (uint32_t)*(const uint16_t*)(rec + v_code_off<D>(tt, d + 4)) << 16;
-    put8((T*)a.v + vo + d, w, kv4_scale(rec[kv4_v_scales(D) + it * 16 + tt]));
+  for (int i = 0; i < NI; ++i) {
+    uint8_t* rec;
+    int tt;
+    live[i] = locate<D, BLOCKS>(a, tile, lane / LPR * NI + i, h, &ko[i], &vo[i], &rec, &tt);
+    if (live[i]) {
+      kw[i] = *(const uint32_t*)(rec + k_code_off<D>(tt, d));
+      if constexpr (D == 128)
+        vw[i] = *(const uint32_t*)(rec + v_code_off<D>(tt, d));
+      else
+        vw[i] = *(const uint16_t*)(rec + v_code_off<D>(tt, d)) | (uint32_t)*(const uint16_t*)(rec + v_code_off<D>(tt, d + 4)) << 16;
+      ks[i] = rec[kv4_k_scales(D) + d / kKv4Group * 16 + tt];
+      vs[i] = rec[kv4_v_scales(D) + d / kKv4Group * 16 + tt];
+    }
   }
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    if (live[i]) {
+      put8((T*)a.k + ko[i] + d, kw[i], kv4_scale(ks[i]));
+      put8((T*)a.v + vo[i] + d, vw[i], kv4_scale(vs[i]));
+    }
 }
 
 }  // namespace
