@@ -18,8 +18,10 @@ namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 constexpr float kNegInf = -__builtin_huge_valf();
-// Requests of more rows per KV head than this take the kernel for many rows (bfloat16).
-constexpr int kKv4FewRows = 64;
+// Requests of more rows per KV head than this take the kernel for many rows (bfloat16).  Measured on both, few / many:
+// 80 rows over 16384 keys (2 requests of 8 heads) 38.5 / 53 us, 96 rows over 16384 (8 of 2) 36 / 55, 128 over 16384 (8
+// of 2) 43 / 58, 128 over 32768 (1 of 8) 46 / 44.
+constexpr int kKv4FewRows = 128;
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8_t, (u32x4_t){a, b, c, d});
@@ -136,7 +138,7 @@ struct Request {
     len = max(min(a.lens[r], a.max_keys), 0);
     rows = nq * a.G;
     off = len - nq;
-    split = kv4_split(rows, len);
+    split = kv4_split(rows, len, a.Hkv);
   }
 };
 
@@ -801,7 +803,7 @@ static hipError_t launch_kv4(const Kv4AttnK& a, hipStream_t s) {
                        a, tiles);
   }
   if (splits > 1) {
-    const int64_t part = rows < kKv4PartRows ? rows : kKv4PartRows;
+    const int64_t part = std::min<int64_t>(rows, kKv4Parts / 2);
     const unsigned wgs = (unsigned)(part < 64 ? part : 64);
     hipLaunchKernelGGL((kv4_merge_kernel<T, D>), dim3(wgs * a.Hkv, (unsigned)a.n_req), dim3(256), 0, s, a);
   }

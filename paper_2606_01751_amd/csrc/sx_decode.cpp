@@ -145,7 +145,7 @@ sx_status check_norm(const void* gamma_q, const void* gamma_k, float eps) {
 }
 
 int64_t workspace_of(const sx_layer_desc* d, int32_t n_requests, int32_t max_q, int32_t max_seqlen, int64_t* part_rows) {
-  const int64_t rows = sx::kv4_part_rows((int64_t)max_q * (d->n_q_heads / d->n_kv_heads), max_seqlen);
+  const int64_t rows = sx::kv4_part_rows((int64_t)max_q * (d->n_q_heads / d->n_kv_heads), max_seqlen, d->n_kv_heads);
   *part_rows = rows;
   return (int64_t)n_requests * d->n_kv_heads * rows * (d->head_dim * 4 + 8);
 }
@@ -336,7 +336,7 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   if (max_q > total_q) max_q = total_q;
   if ((int64_t)max_q * G >= ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_q %d too large", max_q);
   if (max_seqlen > ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_seqlen above 2^30");
-  const int64_t tiles = std::max<int64_t>((max_q * G + 255) / 256, std::min<int64_t>((max_q * G + 15) / 16, esize(desc) == 4 ? INT32_MAX : 4));
+  const int64_t tiles = std::max<int64_t>((max_q * G + 255) / 256, std::min<int64_t>((max_q * G + 15) / 16, esize(desc) == 4 ? INT32_MAX : 8));   // (of 256 and 16 rows)
   if (n_requests > kMaxRequests || tiles * desc->n_kv_heads * n_requests * 512 >= kMaxThreads)
     return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: %d requests of %d query tokens exceed one launch", n_requests, max_q);
   int64_t part_rows;

@@ -1,6 +1,8 @@
 // Internal declarations of the decoding calls (include/sx_decode.h), shared by their host side and kernels.
 #pragma once
 
+#include <algorithm>
+
 #include "sx_decode.h"
 #include "sx_internal.h"
 
@@ -15,36 +17,41 @@ __host__ __device__ constexpr int kv4_v_scales(int d) { return 16 * d + d / 2; }
 
 // ---- split of a request's keys over workgroups ----
 // A request of `rows` query rows per KV head (tokens x group) and `len` keys is cut into chunks of equal
-// length, by its own sizes alone, so that its result does not depend on the rest of the batch: at least
-// kKv4Chunk keys each, at most kKv4Splits of them, and at most kKv4PartRows partial rows in all (few rows
-// need the split to fill the chip; many rows fill it by themselves).
+// length, by its own sizes and the head count alone, so that its result does not depend on the rest of the
+// batch: at least kKv4Chunk keys each, at most kKv4Splits of them, and at most kKv4Parts parts (rows x heads x
+// chunks), which is a workgroup of 256 rows for each of 256 compute units: more rows fill the chip unsplit.  17 to
+// 255 rows count as 256 (128 rows over 65536 keys, 8 heads: 68 us in 32 chunks, 78 in 64); up to 16 as 16.
+// kKv4Chunk: 64 requests of up to 8192 keys 51.7 us at 1024, 55.3 at 512, 53.8 at 2048; 256 requests of 1024 keys
+// 61, 91 and 61 us.
 constexpr int kKv4Chunk = 1024;
 constexpr int kKv4Splits = 64;
-constexpr int kKv4PartRows = 4096;
+constexpr int kKv4Parts = 65536;
 constexpr int kKv4Step = 128;    // a chunk's length is a multiple of this
 struct Kv4Split {
   int n, keys;   // chunks, and keys of each but the last
 };
-__host__ __device__ inline Kv4Split kv4_split(int rows, int len) {   // (32-bit unsigned divisions: len < 2^30 + 1)
-  const uint32_t cap = rows <= 16 ? kKv4PartRows / 16 : (uint32_t)kKv4PartRows / (uint32_t)rows;
-  const uint32_t most = cap < 1 ? 1 : cap > kKv4Splits ? kKv4Splits : cap;
+__host__ __device__ inline uint32_t kv4_most_chunks(uint32_t rows, uint32_t heads) {
+  const uint32_t counted = rows <= 16 ? 16 : rows <= 256 ? 256 : rows;
+  const uint32_t n = kKv4Parts / counted / heads;
+  return n < 1 ? 1 : n > kKv4Splits ? kKv4Splits : n;
+}
+__host__ __device__ inline Kv4Split kv4_split(int rows, int len, int heads) {   // (32-bit divisions: len <= 2^30)
+  const uint32_t most = kv4_most_chunks(rows, heads);
   uint32_t n = ((uint32_t)len + kKv4Chunk - 1) / kKv4Chunk;
   n = n < 1 ? 1 : n > most ? most : n;
   const uint32_t keys = (((uint32_t)len + n - 1) / n + kKv4Step - 1) / kKv4Step * kKv4Step;
   const uint32_t used = keys > 0 ? ((uint32_t)len + keys - 1) / keys : 1;
   return {(int)(used < 1 ? 1 : used), (int)keys};
 }
-// most chunks, and most partial rows (rows x chunks, where there is more than one chunk), of a request of
+// most chunks, and most partial rows per head (rows x chunks, where there is more than one chunk), of a request of
 // at most `rows` rows and `len` keys
 inline int kv4_max_chunks(int len) {
   const int64_t n = ((int64_t)len + kKv4Chunk - 1) / kKv4Chunk;
   return (int)(n < 1 ? 1 : n > kKv4Splits ? kKv4Splits : n);
 }
-inline int64_t kv4_part_rows(int64_t rows, int len) {
-  const int c = kv4_max_chunks(len);
-  if (c <= 1) return 0;
-  const int64_t n = (rows < kKv4PartRows ? rows : kKv4PartRows) * c;
-  return n < kKv4PartRows ? n : kKv4PartRows;
+inline int64_t kv4_part_rows(int64_t rows, int len, int heads) {
+  const int64_t c = kv4_max_chunks(len), cap = std::max(kKv4Parts / heads, 16);
+  return c <= 1 ? 0 : std::min(rows * c, cap);   // (more than one chunk: rows x heads x chunks <= kKv4Parts)
 }
 
 struct AppendSlotsK {

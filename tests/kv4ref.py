@@ -92,7 +92,7 @@ def attention(q, cu, lens, kv, scale):
     arithmetic may be off before the output's own rounding -- a score is a sum of d products and a base-2 exponent formed
     from it (relative 2^-24 each), so a probability is off by at most ds = scale * (d + 4) 2^-24 max_j sum |q k_j| + 2^-22
     (max |s| + 1) relative; numerator and denominator take that, their own sums of up to n terms (n 2^-24), the parts of a
-    probability (2^-16) and the final division (2^-22): twice the sum, times sum p |v|.  bfloat16 requests of more than 64
+    probability (2^-16) and the final division (2^-22): twice the sum, times sum p |v|.  bfloat16 requests of more than 128
     rows (query tokens x heads of the group) take a probability in one part: the numerator's p are each off by half a
     bfloat16 step, 2^-8 relative, the denominator's are not, so 2^-8 sum p |v| comes on top."""
     n, hq, d = q.shape
@@ -123,7 +123,7 @@ def attention(q, cu, lens, kv, scale):
             mag = torch.where(see, qh.abs() @ kh.nan_to_num().abs().t(), torch.zeros_like(s)).amax(-1) * scale
             fin = torch.where(see & torch.isfinite(s), s.abs(), torch.zeros_like(s)).amax(-1)
             ds = mag * (d + 4) * 2.0 ** -24 + 2.0 ** -22 * (fin + 1)
-            one_part = 2.0 ** -8 if q.dtype is torch.bfloat16 and nq * grp > 64 else 0.0
+            one_part = 2.0 ** -8 if q.dtype is torch.bfloat16 and nq * grp > 128 else 0.0
             bound[q0:q0 + nq, h] *= 2 * (ds + m * 2.0 ** -24 + 2.0 ** -16 + 2.0 ** -22)[:, None] + one_part
             lse_bound[q0:q0 + nq, h] = 2 * (ds + m * 2.0 ** -24 + 2.0 ** -22 * (1 + lse[q0:q0 + nq, h].abs().nan_to_num(0, 0, 0)))
     return out, lse, bound, lse_bound
