@@ -9,6 +9,7 @@
 // LDS until the waves of a workgroup, which take the steps of a chunk of keys in turn, add up their parts.
 // Softmax statistics and sums are float32; a probability goes into the product as two bfloat16 parts (float32
 // q: three, and q itself in three), so what is lost there is below the rounding of the output.
+#include <algorithm>
 #include <type_traits>
 
 #include "sx_kv4_device.h"
@@ -142,6 +143,58 @@ struct Request {
   }
 };
 
+// What a workgroup does: items are (request, chunk of its keys, tile of its rows) of one KV head, numbered request by
+// request, a request's tiles fastest.  The host knows bounds only, and a workgroup without an item costs its dispatch
+// and its look at the lengths, so where a launch for every possible item would be large, a smaller one finds its items
+// by the requests' item counts.  Every thread of the workgroup calls this; false: no such item.
+template <int THREADS, typename CountF>
+__device__ __forceinline__ bool find_item(const Kv4AttnK& a, uint32_t item, CountF count, int* request, uint32_t* in_request) {
+  __shared__ uint32_t total[THREADS / 64];
+  __shared__ int s_request;
+  __shared__ uint32_t s_item;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t base = 0;
+  for (int r0 = 0; r0 < a.n_req; r0 += THREADS) {
+    const int r = r0 + (int)threadIdx.x;
+    const uint32_t n = r < a.n_req ? count(Request(a, r)) : 0;
+    uint32_t x = n;   // inclusive prefix over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(x, o, 64);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) total[wave] = x;
+    __syncthreads();
+    uint32_t before = base, all = base;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) before += total[w];
+      all += total[w];
+    }
+    if (item - (before + x - n) < n) {   // (unsigned: item below its first wraps)
+      s_request = r;
+      s_item = item - (before + x - n);
+    }
+    __syncthreads();
+    if (item < all) {
+      *request = __builtin_amdgcn_readfirstlane(s_request);
+      *in_request = __builtin_amdgcn_readfirstlane(s_item);
+      return true;
+    }
+    base = all;
+  }
+  return false;
+}
+
+// The kernel's first argument, read from the kernel-argument segment through a pointer the compiler cannot follow, so
+// that a kernel that loops over items keeps nothing of it in registers from one to the next.
+__device__ __forceinline__ Kv4AttnK item_args() {
+  typedef const __attribute__((address_space(4))) char* ArgPtr;
+  ArgPtr p = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Kv4AttnK*)(const char*)p;
+}
+
 // Halves of the pairs (x: one of two keys, y: the other) as the two keys of one column: the low or high ones.
 template <int ODD>
 __device__ __forceinline__ uint32_t halves(uint32_t x, uint32_t y) {
@@ -167,7 +220,7 @@ __device__ __forceinline__ void for_each(F&& f) {
 // TB/s; a plain streaming read reaches 5.5 - 6.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+__device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& q, int r, int h, int tile, int c) {
   constexpr int NC = D / 32;                  // 32-element pieces of a row
   constexpr int NU = D / 16;                  // 16-column tiles of V
   constexpr int NQ = sizeof(T) == 4 ? 3 : 1;  // bfloat16 parts of a query element, and of a probability
@@ -175,16 +228,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) vo
   constexpr int OP = D + 4;                   // LDS row pitch
   __shared__ __attribute__((aligned(16))) float so[NW][16][OP];
   __shared__ float sm[NW][16], sl[NW][16];
-  // chunks slowest: workgroups beyond a request's last chunk end at once, and between live ones they would put
-  // these on a few shader engines
-  const int c = blockIdx.y;
-  uint32_t idx = blockIdx.x;
-  const int h = idx % (uint32_t)a.Hkv;
-  idx /= (uint32_t)a.Hkv;
-  const int tile = idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;
-  const Request q(a, r);
   const int row0 = tile * 16 * MT;
-  if (row0 >= q.rows || c >= q.split.n || (sizeof(T) == 2 && q.rows > kKv4FewRows)) return;
   const int G = a.G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -407,6 +451,37 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) vo
   }
 }
 
+template <typename T, int MT>
+__device__ __forceinline__ uint32_t few_tiles(const Request& q) {   // (0: the request is not for this kernel)
+  return sizeof(T) == 2 && q.rows > kKv4FewRows ? 0u : (uint32_t)(q.rows + 16 * MT - 1) / (16 * MT);
+}
+
+// A workgroup for every possible item: x = KV head, tile, request, y = chunk.  Chunks slowest: workgroups beyond a
+// request's last chunk end at once, and between live ones they would put these on a few shader engines.
+template <typename T, int D, int MT, int NW>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+  const int h = blockIdx.x % (uint32_t)a.Hkv, c = blockIdx.y;
+  const uint32_t idx = blockIdx.x / (uint32_t)a.Hkv, tile = idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;
+  const Request q(a, r);
+  if (tile < few_tiles<T, MT>(q) && c < q.split.n) few_rows_item<T, D, MT, NW>(a, q, r, h, tile, c);
+}
+
+// Workgroups that take items in turn.
+template <typename T, int D, int MT, int NW>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_items_kernel(Kv4AttnK ka) {
+  const int h = blockIdx.x % (uint32_t)ka.Hkv;
+  for (uint32_t item = blockIdx.x / (uint32_t)ka.Hkv;; item += gridDim.x / (uint32_t)ka.Hkv) {
+    const Kv4AttnK a = item_args();
+    int r;
+    uint32_t at;
+    if (!find_item<NW * 64>(a, item, [&](const Request& q) { return few_tiles<T, MT>(q) * q.split.n; }, &r, &at)) return;
+    const Request q(a, r);
+    const uint32_t n = few_tiles<T, MT>(q);
+    few_rows_item<T, D, MT, NW>(a, q, r, h, at % n, at / n);
+    __syncthreads();   // (the item's LDS is free again)
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // Many query rows (bfloat16): one workgroup of 8 waves takes 256 columns (32 a wave) of one KV head over one
 // chunk of keys, in tiles of 64 keys = 4 blocks.  Each wave turns the K or the V of one block of the tile into
@@ -430,21 +505,14 @@ constexpr int kWideCols = 256;
 constexpr int kWideKeys = 64;
 
 template <int D>
-__global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int tiles) {
+__device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request& q, int r, int h, int tile, int c) {
   constexpr int NS = D / 16;          // 16-element slices of a key
   constexpr int ND = D / 32;          // 32-column tiles of the output; dwords of codes per lane
   constexpr int TILEB = kWideKeys * D * 2;
   constexpr int NBUF = 3;
   __shared__ __attribute__((aligned(1024))) char smem[2 * NBUF * TILEB];   // [buffer][K], [buffer][V]
   __shared__ int s_nan[NBUF];         // NaN groups among the values of the buffer's tile (replaced by zero)
-  const int c = blockIdx.y;           // (slowest, as above)
-  uint32_t idx = blockIdx.x;
-  const int h = idx % (uint32_t)a.Hkv;
-  idx /= (uint32_t)a.Hkv;
-  const int tile = tiles - 1 - idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;   // later rows see more keys: first
-  const Request q(a, r);
   const int row0 = tile * kWideCols;
-  if (q.rows <= kKv4FewRows || row0 >= q.rows || c >= q.split.n) return;
   const int G = a.G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -712,100 +780,156 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK a, int t
   }
 }
 
-// The parts of split requests.  A wave takes the chunks w, w + W, ... of a row (their loads all in flight at
-// once): W = 1 and four rows a workgroup for up to 16 chunks, else W = 4 waves a row, added in order.  One row
-// a workgroup for any number of chunks took 8.4 us where 1792 rows had 5 chunks each.
-template <typename T, int D>
+// A workgroup for every possible item, or (LOOP) fewer that take items in turn.
+template <int D, bool LOOP>
+__global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK ka) {
+  const int h = blockIdx.x % (uint32_t)ka.Hkv;
+  auto tiles_of = [](const Request& q) {
+    return q.rows > kKv4FewRows ? (uint32_t)(q.rows + kWideCols - 1) / kWideCols : 0u;
+  };
+  auto run = [&](const Kv4AttnK& a, uint32_t item) __attribute__((always_inline)) {
+    int r;
+    uint32_t at;
+    if (!find_item<512>(a, item, [&](const Request& q) { return tiles_of(q) * q.split.n; }, &r, &at)) return false;
+    const Request q(a, r);
+    const uint32_t n = tiles_of(q);
+    many_rows_item<D>(a, q, r, h, n - 1 - at % n, at / n);   // later rows see more keys: first
+    return true;
+  };
+  if constexpr (LOOP) {
+    for (uint32_t item = blockIdx.x / (uint32_t)ka.Hkv; run(item_args(), item); item += gridDim.x / (uint32_t)ka.Hkv) __syncthreads();
+  } else {
+    run(ka, blockIdx.x / (uint32_t)ka.Hkv);
+  }
+}
+
+// The parts of split requests: a wave per (token, head), 32 chunks' loads in flight at once, or (FOUR) four waves, a
+// workgroup, with 16 each.  The chunks c, c + 4, .. are added in order, then the four sums, in both.
+template <typename T, int D, bool FOUR>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   constexpr int E = D / 64;                  // elements per lane
-  constexpr int PER = kKv4Splits / 4;        // most chunks per wave
-  __shared__ float so[4][D];
-  const int r = blockIdx.y, h = blockIdx.x % (uint32_t)a.Hkv;
-  const Request q(a, r);
-  if (q.split.n == 1) return;
-  const int G = a.G, lane = threadIdx.x & 63, n = q.split.n;   // n <= 64: a chunk per lane
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool alone = n <= PER;               // one wave a row
-  const int first = blockIdx.x / (uint32_t)a.Hkv, step = gridDim.x / (uint32_t)a.Hkv;
-  for (int base_row = alone ? first * 4 : first; base_row < q.rows; base_row += alone ? step * 4 : step) {
-    const int row = min(alone ? base_row + wave : base_row, q.rows - 1);
-    const int c0 = alone ? 0 : wave, cs = alone ? 1 : 4;
-    const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + row;
-    const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);
-    float x[PER][E];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = c0 + cs * i;
-      const float* src = a.part + (at + (int64_t)c * q.rows) * D + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[i][e] = c < n ? src[e] : 0.0f;
+  constexpr int STEP = FOUR ? 4 : 1, BATCH = FOUR ? kKv4Splits / 4 : 32;
+  __shared__ float so[FOUR ? 4 : 1][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = FOUR ? blockIdx.y : blockIdx.y * 4 + wave;
+  if (head >= a.Hq) return;
+  const int h = head / (uint32_t)a.G;
+  for (int token = blockIdx.x; token < a.total_q; token += gridDim.x) {
+    const int r = __builtin_amdgcn_readfirstlane(lower_bound_wave(a.cu + 1, a.n_req, token + 1, lane));
+    if (r >= a.n_req) return;                // behind the last sequence
+    const Request q(a, r);
+    const int i = token - q.q0, n = q.split.n;
+    if (n == 1) {                            // on to the next request's tokens
+      if (q.nq - i > (int)gridDim.x) token += (q.nq - i - 1) / gridDim.x * gridDim.x;
+      continue;
     }
+    if (i < 0 || i >= q.nq) continue;
+    const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + i * a.G + head % (uint32_t)a.G;
+    const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);   // n <= 64: a chunk per lane
+    const float* src = a.part + at * D + lane * E;
     const float mt = wave_max(ml.x);
-    const float base = mt == kNegInf ? 0.0f : mt;
-    const float f = __builtin_amdgcn_exp2f(ml.x - base);
+    const float f = __builtin_amdgcn_exp2f(ml.x - (mt == kNegInf ? 0.0f : mt));
     float lt = ml.y * f;                     // (a fixed tree over the lanes)
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) lt += __shfl_xor(lt, s, 64);
-    float acc[E];
+    float acc[4][E];                         // (FOUR: the first of them)
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+    for (int w = 0; w < 4; ++w)
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = c0 + cs * i;
-      const float fc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), c & 63));
+      for (int e = 0; e < E; ++e) acc[w][e] = 0.0f;
+    for (int c0 = FOUR ? wave : 0; c0 < n; c0 += BATCH * STEP) {
+      float x[BATCH][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x[i][e], c < n ? fc : 0.0f, acc[e]);
-    }
-    if (!alone) {
+      for (int p = 0; p < BATCH; ++p)
 #pragma unroll
-      for (int e = 0; e < E; ++e) so[wave][lane * E + e] = acc[e];
-      __syncthreads();
+        for (int e = 0; e < E; ++e) x[p][e] = c0 + p * STEP < n ? src[(int64_t)(c0 + p * STEP) * q.rows * D + e] : 0.0f;
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        acc[e] = (so[0][lane * E + e] + so[1][lane * E + e]) + (so[2][lane * E + e] + so[3][lane * E + e]);
-      __syncthreads();
-    }
-    if (alone ? base_row + wave < q.rows : wave == 0) {
-      const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-      const int64_t to = (int64_t)(q.q0 + row / G) * a.Hq + h * G + row % G;
-      T* dst = (T*)a.out + to * D + lane * E;
-      if constexpr (E == 1) {
-        if constexpr (sizeof(T) == 2) *dst = (uint16_t)pack_bf16x2(acc[0] * inv, 0.0f);
-        else *dst = acc[0] * inv;
-      } else {
-        if constexpr (sizeof(T) == 2) *(uint32_t*)dst = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-        else *(float2*)dst = make_float2(acc[0] * inv, acc[1] * inv);
+      for (int p = 0; p < BATCH; ++p) {      // (behind the last chunk: f = 2^-inf = 0)
+        const float fc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), c0 + p * STEP));
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[FOUR ? 0 : p & 3][e] = __builtin_fmaf(x[p][e], fc, acc[FOUR ? 0 : p & 3][e]);
       }
-      if (a.lse && lane == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
     }
+    if constexpr (FOUR) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) so[wave][lane * E + e] = acc[0][e];
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[w][e] = so[w][lane * E + e];
+      __syncthreads();
+      if (wave != 0) continue;
+    }
+    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+    const int64_t to = (int64_t)token * a.Hq + head;
+    T* dst = (T*)a.out + to * D + lane * E;
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = ((acc[0][e] + acc[1][e]) + (acc[2][e] + acc[3][e])) * inv;
+    if constexpr (E == 1) {
+      if constexpr (sizeof(T) == 2) *dst = (uint16_t)pack_bf16x2(v[0], 0.0f);
+      else *dst = v[0];
+    } else {
+      if constexpr (sizeof(T) == 2) *(uint32_t*)dst = pack_bf16x2(v[0], v[1]);
+      else *(float2*)dst = make_float2(v[0], v[1]);
+    }
+    if (a.lse && lane == 0) a.lse[to] = (mt + __builtin_amdgcn_logf(lt)) * 0.69314718055994530942f;
   }
 }
 
 }  // namespace
 
+// Workgroups of a launch.  64 requests of 1000 keys cost 15.6 us where the host says 1000 keys, but took 43 where it
+// says 131072 and every possible chunk had a workgroup, 305 with bounds of 512 queries beside it.
+constexpr int64_t kDirectGroups = 4096;   // most workgroups launched for possible items
+constexpr int64_t kFewGroups = 2048;      // ... that take items in turn: a few a compute unit
+constexpr int64_t kWideDirect = 2048;     // the same of the kernel for many rows, of which one fits a compute unit
+constexpr int64_t kWideGroups = 512;
+constexpr int64_t kMergeGroups = 4096;
+
+template <typename T, int D, int MT>
+static void launch_few(const Kv4AttnK& a, int64_t rows, int splits, hipStream_t s) {
+  const int64_t tiles = (rows + 16 * MT - 1) / (16 * MT), all = tiles * a.Hkv * a.n_req;
+  if (all * splits <= kDirectGroups) {
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4>), dim3((unsigned)all, (unsigned)splits), dim3(256), 0, s, a, (int)tiles);
+    return;
+  }
+  // at most so many tiles by the rows of q, too
+  const int64_t most = std::min(tiles * a.n_req, (int64_t)a.total_q * a.G / (16 * MT) + a.n_req) * splits;
+  const int64_t items = std::max<int64_t>(1, std::min(most, kFewGroups / a.Hkv));
+  hipLaunchKernelGGL((kv4_attn_items_kernel<T, D, MT, 4>), dim3((unsigned)(items * a.Hkv)), dim3(256), 0, s, a);
+}
+
 template <typename T, int D>
 static hipError_t launch_kv4(const Kv4AttnK& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
+  const int64_t rows = (int64_t)a.max_q * a.G;
   const int splits = kv4_max_chunks(a.max_keys);
   if constexpr (sizeof(T) == 2) {
     if (rows > kKv4FewRows) {
-      const int wide = (int)((rows + kWideCols - 1) / kWideCols);
-      hipLaunchKernelGGL((kv4_attn_wide_kernel<D>), dim3((unsigned)(wide * a.Hkv * a.n_req), (unsigned)splits), dim3(512), 0, s, a,
-                         wide);
+      // a request of t tiles in n > 1 chunks has rows x heads x n <= kKv4Parts, so t n <= 2 x 256 / heads
+      const int64_t requests = std::min<int64_t>(a.n_req, (int64_t)a.total_q * a.G / (kKv4FewRows + 1) + 1);
+      const int64_t all_tiles = (int64_t)a.total_q * a.G / kWideCols + requests;
+      const int64_t n = std::min<int64_t>(splits, kv4_most_chunks(kKv4FewRows + 1, a.Hkv));
+      const int64_t most = std::min(all_tiles * n, all_tiles + requests * (2 * kKv4Parts / kWideCols / a.Hkv + 1)) * a.Hkv;
+      if (most <= kWideDirect)
+        hipLaunchKernelGGL((kv4_attn_wide_kernel<D, false>), dim3((unsigned)most), dim3(512), 0, s, a);
+      else
+        hipLaunchKernelGGL((kv4_attn_wide_kernel<D, true>), dim3((unsigned)(std::max<int64_t>(1, kWideGroups / a.Hkv) * a.Hkv)),
+                           dim3(512), 0, s, a);
     }
   }
-  const int64_t few = sizeof(T) == 2 && rows > kKv4FewRows ? kKv4FewRows : rows;
-  if (few <= 16) {
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 1, 4>), dim3((unsigned)(a.Hkv * a.n_req), (unsigned)splits), dim3(256), 0, s, a, 1);
-  } else {
-    const int tiles = (int)((few + 31) / 32);
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 4>), dim3((unsigned)(tiles * a.Hkv * a.n_req), (unsigned)splits), dim3(256), 0, s,
-                       a, tiles);
-  }
+  const int64_t few = sizeof(T) == 2 ? std::min<int64_t>(rows, kKv4FewRows) : rows;
+  if (few <= 16) launch_few<T, D, 1>(a, few, splits, s);
+  else launch_few<T, D, 2>(a, few, splits, s);
   if (splits > 1) {
-    const int64_t part = std::min<int64_t>(rows, kKv4Parts / 2);
-    const unsigned wgs = (unsigned)(part < 64 ? part : 64);
-    hipLaunchKernelGGL((kv4_merge_kernel<T, D>), dim3(wgs * a.Hkv, (unsigned)a.n_req), dim3(256), 0, s, a);
+    // few rows of many chunks: four waves each (one token of 32 heads in 64 chunks: 4.5 us, 8.6 in one)
+    const bool four = splits > kKv4Splits / 4 && (int64_t)a.total_q * a.Hq <= kMergeGroups / 4;
+    const int64_t groups = four ? a.Hq : (a.Hq + 3) / 4;
+    const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(a.total_q, kMergeGroups / groups));
+    const dim3 grid((unsigned)tokens, (unsigned)groups);
+    if (four) hipLaunchKernelGGL((kv4_merge_kernel<T, D, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv4_merge_kernel<T, D, false>), grid, dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

@@ -336,9 +336,7 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   if (max_q > total_q) max_q = total_q;
   if ((int64_t)max_q * G >= ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_q %d too large", max_q);
   if (max_seqlen > ((int64_t)1 << 30)) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: max_seqlen above 2^30");
-  const int64_t tiles = std::max<int64_t>((max_q * G + 255) / 256, std::min<int64_t>((max_q * G + 15) / 16, esize(desc) == 4 ? INT32_MAX : 8));   // (of 256 and 16 rows)
-  if (n_requests > kMaxRequests || tiles * desc->n_kv_heads * n_requests * 512 >= kMaxThreads)
-    return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: %d requests of %d query tokens exceed one launch", n_requests, max_q);
+  if (n_requests > kMaxRequests) return reportf(SX_EUNSUPPORTED, "sx_kv4_attn: more than %d requests", kMaxRequests);
   int64_t part_rows;
   const int64_t need = workspace_of(desc, n_requests, max_q, max_seqlen, &part_rows);
   if (need > 0 && !workspace) return reportf(SX_EINVAL, "workspace is NULL");

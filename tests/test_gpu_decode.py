@@ -431,6 +431,45 @@ def test_kv4_attn_split_rows(hq, hkv, d, dtype, nq, nk):
     Batch([(nq, nk), (1, nk // 2)], hq, hkv, d, dtype, seed=nk).check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_kv4_attn_loose_bounds_and_many_requests(dtype):
+    # with loose bounds the workgroups look for their items: requests of no token, no key, few rows and many, more of
+    # them than a workgroup has threads; the same bits as each request by itself, and right
+    g = torch.Generator().manual_seed(3)
+    sizes = [(1, int(n)) for n in torch.randint(0, 90, (560,), generator=g)]
+    for i in range(0, 560, 14):
+        sizes[i] = [(0, 30), (45, 150), (3, 2500), (33, 1200), (40, 9), (1, 5000)][i // 14 % 6]
+    b = Batch(sizes, 8, 2, 64, dtype, seed=12)
+    out, lse = b.check(max_q=4096, max_keys=131072)
+    tight, tight_lse = b.run()
+    assert torch.equal(out, tight) and torch.equal(lse, tight_lse)
+    for r in [14 * i for i in range(13)] + [1, 2, 255, 256, 559]:
+        nq, nk = sizes[r]
+        if nq == 0:
+            continue
+        o = torch.empty_like(b.q[b.cu[r]:b.cu[r + 1]])
+        ws = torch.empty(max(16, sx.kv4_attn_workspace(b.desc, 1, nq, max(nk, 1))), dtype=torch.uint8, device="cuda")
+        sx.kv4_attn(b.desc, b.q[b.cu[r]:b.cu[r + 1]].contiguous(), i32([0, nq]), i32([nk]), b.table[r:r + 1].cuda().contiguous(), b.pool,
+                    o, nq, max(nk, 1), ws)
+        assert torch.equal(o, out[b.cu[r]:b.cu[r + 1]]), r
+
+
+def test_kv4_attn_scale_and_empty_table():
+    b = Batch([(3, 70), (1, 20)], 4, 2, 64, "f32", seed=1)
+    b.desc = sx.make_desc(4, 2, 64, "f32", 1e4, softmax_scale=0.3)
+    out = torch.empty_like(b.q)
+    ws = torch.empty(16, dtype=torch.uint8, device="cuda")
+    sx.kv4_attn(b.desc, b.q, i32(b.cu), i32(b.nk), b.table.cuda(), b.pool, out, 3, 70, ws)
+    pool = b.pool.cpu()
+    kv = [R.rows_of(pool, b.table[r], n, 64) for r, n in enumerate(b.nk)]
+    want, _, bound, _ = R.attention(b.q.cpu(), b.cu, b.nk, kv, 0.3)
+    near(out[:4], want[:4], bound[:4], "f32")
+    sx.kv4_attn(b.desc, b.q, i32(b.cu), i32(b.nk), b.table.cuda()[:, :0].contiguous(), b.pool, out, 3, 70, ws)   # no blocks at all
+    assert (out[:4] == 0).all()
+    sx.kv4_attn(b.desc, b.q[:0], i32([0, 0, 0]), i32(b.nk), b.table.cuda(), b.pool, out[:0], 3, 70, None)         # no tokens
+    sx.kv4_attn(b.desc, b.q, i32([0]), i32([]), b.table.cuda()[:0], b.pool, out, 3, 70, None)                     # no requests
+
+
 def test_kv4_attn_lengths_beyond_the_bounds_are_cut():
     # the release library never reads past what the host was told: 2 blocks a row, 20 keys, 3 queries
     b = Batch([(1, 32), (1, 32)], 4, 2, 64, "bf16", seed=3)
