@@ -9,7 +9,7 @@
 // Row lists (row-list layout of include/sx.h), per request r with n = n_rows[r]:
 //   0 <= n <= T_r; the first min(n, max_rows) rows are in [0, T_r) and strictly ascending.
 // cu_seqlens: cu[0] = 0 and 0 <= cu[r + 1] - cu[r] <= max_seqlen.
-// The decoding calls (include/sx_decode.h): lengths >= 0, indices (slots, block ids) from -1 up to their
+// The decoding calls (include/sx_decode.h): lengths >= 0, indices (slots, block ids; a free list's from 0) from -1 up to their
 // bound, and for the attention cu_q as cu_seqlens, within total_q, and the block table entries of every key.
 // The checks read only in-bounds entries: at most T_r rows of a request's own region.
 #include "sx_kv4.h"
@@ -67,9 +67,9 @@ __global__ __launch_bounds__(256) void check_lengths_kernel(const int32_t* __res
   else if (n < 0 || n > INT32_MAX - c) report_bad(kBadLength, r, r, n);
 }
 
-__global__ __launch_bounds__(256) void check_index_kernel(const int32_t* __restrict__ idx, int n, int64_t limit) {
+__global__ __launch_bounds__(256) void check_index_kernel(const int32_t* __restrict__ idx, int n, int low, int64_t limit) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n && (idx[i] < -1 || idx[i] >= limit)) report_bad(kBadIndex, 0, i, idx[i]);
+  if (i < n && (idx[i] < low || idx[i] >= limit)) report_bad(kBadIndex, 0, i, idx[i]);
 }
 
 __global__ __launch_bounds__(256) void check_kv4_kernel(Kv4AttnK a) {   // one workgroup per request
@@ -120,9 +120,9 @@ hipError_t device_check_lengths(const int32_t* ctx, const int32_t* add, int32_t 
   return read_verdict(s, verdict);
 }
 
-hipError_t device_check_index(const int32_t* idx, int32_t n, int64_t limit, hipStream_t s, int verdict[4]) {
+hipError_t device_check_index(const int32_t* idx, int32_t n, int32_t low, int64_t limit, hipStream_t s, int verdict[4]) {
   hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
-  hipLaunchKernelGGL(check_index_kernel, dim3((unsigned)(((int64_t)n + 255) / 256)), dim3(256), 0, s, idx, n, limit);
+  hipLaunchKernelGGL(check_index_kernel, dim3((unsigned)(((int64_t)n + 255) / 256)), dim3(256), 0, s, idx, n, low, limit);
   return read_verdict(s, verdict);
 }
 

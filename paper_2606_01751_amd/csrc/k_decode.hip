@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
   const int64_t head = a.free_head ? max(a.free_head[0], 0) : 0;
   const uint32_t b = a.block;
   int64_t tok = 0, blk = 0, missing = 0;
-  for (int r0 = 0; r0 < a.n_req; r0 += kSlotRun) {
+  for (int r0 = 0; r0 < a.n_req && (per_request || tok < t1); r0 += kSlotRun) {   // (uniform)
     const int r = r0 + tid;
     const int ctx = r < a.n_req ? max(a.ctx[r], 0) : 0;
     const int add = r < a.n_req ? (a.add ? max(a.add[r], 0) : 1) : 0;

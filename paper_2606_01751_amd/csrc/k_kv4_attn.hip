@@ -326,7 +326,7 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
         for (int e = 0; e < 8; ++e)
           if (id[e >> 2] < 0 || kb + 16 * (e >> 2) + 4 * lg + (e & 3) > lim[t]) s[e] = kNegInf;
       }
-      // the maximum is raised only when a probability would reach 2^64 (or is not a number): the same softmax,
+      // the maximum is raised only when a probability would reach 2^24 (or is not a number): the same softmax,
       // and no maximum over the lanes in most steps
       float p[8], psum;
       auto expo = [&](float neg) {
@@ -338,7 +338,7 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
         }
       };
       expo(-m[t]);
-      if (__any(!(psum < 0x1p64f))) {
+      if (__any(!(psum < 0x1p24f))) {
         float top = s[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
@@ -498,8 +498,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_item
 // Probabilities are rounded to bfloat16 once, as in full and sparse attention: the error of a result, 2^-9 of its
 // typical size, is that of its own rounding (0.0024 relative with both, 0.0017 with the output's alone), and two
 // parts cost 1378 us where one costs 964.  Sums and statistics are float32; the running maximum is raised only
-// when a probability would reach 2^64.
-// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 964 us, 1.10 PFLOP/s; the kernel for few rows took 11.4 ms.
+// when a probability would reach 2^24.
+// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 940 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
+// 1.26); the kernel for few rows took 11.4 ms.  Deeper operand reads (2 to 8 MFMAs ahead) change nothing, without its
+// softmax or its conversion the loop takes 970 and 837 us: bound by the matrix phase, whose MFMAs run at about that rate.
 // ---------------------------------------------------------------------------------------------
 constexpr int kWideCols = 256;
 constexpr int kWideKeys = 64;
@@ -678,7 +680,7 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
       }
     };
     expo(-m_run);
-    if (__ballot(!(psum < 0x1p64f))) {
+    if (__ballot(!(psum < 0x1p24f))) {
       float mx = sacc[0][0];
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)

@@ -38,7 +38,7 @@ sx_status check_rows_arg(const sx_layer_desc* d, const char* name, const void* p
 }
 
 const char* kWhat[] = {"", "", "", "", "cu_q[0] is not 0", "a request's query tokens are negative or above max_q",
-                       "a length is negative or out of range", "an index is below -1 or out of range",
+                       "a length is negative or out of range", "an index is out of range",
                        "a block table entry is below -1 or out of range", "cu_q ends behind total_q"};
 
 sx_status verdict_status(hipError_t e, const int v[4], const char* who) {
@@ -48,10 +48,10 @@ sx_status verdict_status(hipError_t e, const int v[4], const char* who) {
   return SX_OK;
 }
 
-sx_status index_ok(const int32_t* idx, int32_t n, int64_t limit, void* stream, const char* who) {
+sx_status index_ok(const int32_t* idx, int32_t n, int64_t limit, void* stream, const char* who, int32_t low = -1) {
   if (!SX_DEVICE_CHECKS || n == 0) return SX_OK;
   int v[4] = {0, 0, 0, 0};
-  const hipError_t e = sx::device_check_index(idx, n, limit, (hipStream_t)stream, v);
+  const hipError_t e = sx::device_check_index(idx, n, low, limit, (hipStream_t)stream, v);
   return verdict_status(e, v, who);
 }
 
@@ -181,7 +181,7 @@ sx_status sx_append_slots(const int32_t* ctx_lens, const int32_t* new_lens, int3
     hipError_t e = sx::device_check_lengths(ctx_lens, new_lens, n_requests, (hipStream_t)stream, v);
     sx_status st = verdict_status(e, v, "sx_append_slots");
     if (st != SX_OK) return st;
-    if ((st = index_ok(free_blocks, n_free, (int64_t)INT32_MAX / block_size, stream, "sx_append_slots")) != SX_OK) return st;
+    if ((st = index_ok(free_blocks, n_free, (int64_t)INT32_MAX / block_size, stream, "sx_append_slots", 0)) != SX_OK) return st;
   }
   sx::AppendSlotsK a{};
   a.ctx = ctx_lens;
@@ -210,6 +210,8 @@ sx_status sx_qk_norm_rope(const sx_layer_desc* desc, const void* q, int64_t q_ld
   if (st != SX_OK) return st;
   if (n_tokens < 0) return reportf(SX_EINVAL, "n_tokens must be >= 0");
   if (n_tokens == 0) return SX_OK;
+  // (a workgroup of 256 threads takes 512 / head_dim tokens)
+  if ((int64_t)n_tokens * (desc->head_dim / 2) >= kMaxThreads) return reportf(SX_EUNSUPPORTED, "%d tokens exceed one launch", n_tokens);
   if ((st = check_rows_arg(desc, "q", q, q_ld, desc->n_q_heads)) != SX_OK) return st;
   if ((st = check_rows_arg(desc, "k", k, k_ld, desc->n_kv_heads)) != SX_OK) return st;
   if ((st = check_rows_arg(desc, "q_out", q_out, q_out_ld, desc->n_q_heads)) != SX_OK) return st;

@@ -123,7 +123,7 @@ hipError_t launch_kv4_attn(const Kv4AttnK& a, int D, bool f32, hipStream_t s);
 
 // Checked library: device-side validation (synchronises the stream); verdict as in sx_internal.h.
 hipError_t device_check_lengths(const int32_t* ctx, const int32_t* add, int32_t n_req, hipStream_t s, int verdict[4]);
-hipError_t device_check_index(const int32_t* idx, int32_t n, int64_t limit, hipStream_t s, int verdict[4]);
+hipError_t device_check_index(const int32_t* idx, int32_t n, int32_t low, int64_t limit, hipStream_t s, int verdict[4]);
 hipError_t device_check_kv4(const Kv4AttnK& a, hipStream_t s, int verdict[4]);
 
 }  // namespace sx

@@ -61,7 +61,7 @@ def qk_args(**kw):
     (dict(pos=None), sx.SX_EINVAL, "positions"), (dict(qld=1016), sx.SX_ESHAPE, "between rows"),
     (dict(kld=257), sx.SX_ESHAPE, "between rows"), (dict(q=A + 8), sx.SX_EINVAL, "aligned"),
     (dict(gk=A + 4), sx.SX_EINVAL, "gamma"), (dict(eps=0.0), sx.SX_EINVAL, "eps"), (dict(eps=math.nan), sx.SX_EINVAL, "eps"),
-    (dict(n=-1), sx.SX_EINVAL, "n_tokens"), (dict(qo=A, qold=2048), sx.SX_EINVAL, "in place"),
+    (dict(n=-1), sx.SX_EINVAL, "n_tokens"), (dict(n=(1 << 31) - 1), sx.SX_EUNSUPPORTED, "one launch"), (dict(qo=A, qold=2048), sx.SX_EINVAL, "in place"),
 ])
 def test_qk_norm_rope_refusals(kw, want, text):
     err(sx.lib().sx_qk_norm_rope(ctypes.byref(desc()), *qk_args(**kw)), want, text)

@@ -81,6 +81,14 @@ def test_append_slots_short_lists_and_rooms():
             check_slots(ctx, new, 16, free, head, table.clone(), room)
 
 
+def test_append_slots_most_requests():
+    n = 65536
+    ctx = [(7 * r) % 33 for r in range(n)]
+    new = [1 + (r % 1000 == 3) for r in range(n)]
+    table = torch.arange(n * 3, dtype=torch.int32).view(n, 3)
+    check_slots(ctx, new, 16, list(range(3 * n, 3 * n + 5000)), 0, table, sum(new) + 11)
+
+
 def test_append_slots_one_token_each_and_negative_lengths():
     table = torch.arange(12, dtype=torch.int32).view(3, 4)
     check_slots([15, 16, 0], [1, 1, 1], 16, [20, 21, 22], 0, table, 5, none=True)
