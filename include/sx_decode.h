@@ -63,7 +63,8 @@ extern "C" {
  *   slots        [max_tokens] block * block_size + offset; -1 behind the last one, and for a token
  *                that has no block (list used up, table too narrow, a negative table entry)
  *   state        [2] the free list's next entry, and the number of new tokens that got no slot (0: all
- *                is well; tokens that do not fit into max_tokens count, their blocks stay taken)
+ *                is well; tokens that do not fit into max_tokens count, their blocks are taken and entered
+ *                in block_table all the same)
  * A later step passes state as its free_head.  Outputs must not overlap the inputs or each other
  * (SX_EINVAL), so a loop in a graph copies seq_lens and state back before its next step.
  * One launch.  n_requests <= 65536, block_size >= 1. */

@@ -87,6 +87,11 @@ __global__ __launch_bounds__(kSlotRun) void append_slots_kernel(AppendSlotsK a, 
         const int64_t upto = max(min(min(have + got, (int64_t)a.max_blocks) * b - ctx, (int64_t)add), (int64_t)0);
         const int64_t room = max(min((int64_t)a.max_tokens - c, (int64_t)add), (int64_t)0);
         missing += add - max(min(upto, room) - from, (int64_t)0);
+        if (c + add > a.max_tokens)   // blocks that open behind the room
+          for (int64_t bi = max(have, ((int64_t)a.max_tokens - c + ctx + b - 1) / b); bi < have + need; ++bi) {
+            const int64_t e = f + bi - have;
+            a.table[(int64_t)r * a.max_blocks + bi] = e < a.n_free ? a.free_blocks[e] : -1;
+          }
       }
     } else if (tok + all_tok > t0 && tok < t1) {   // (uniform)
       run.tok[tid] = (int)min(st - add, (int64_t)INT32_MAX);

@@ -166,7 +166,7 @@ def append_slots(ctx, new, b, free, head, table, room):
                 else:
                     f = head + blk - have
                     bid = int(free[f]) if f < len(free) else -1
-                    if i < room and p % b == 0:
+                    if p % b == 0:
                         table[r, blk] = bid
             if i < room:
                 pos[i] = p
