@@ -188,14 +188,16 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNormRopeK a, int pa
   __shared__ __attribute__((aligned(16))) float cs[TB][D / 2], sn[TB][D / 2];
   __shared__ int64_t rows[TB];        // token rows, -1: none
   const int part = blockIdx.x % (uint32_t)parts, n0 = blockIdx.x / (uint32_t)parts * TB;
-  const int live = ROWS ? min(a.n_rows[blockIdx.y], a.max_rows) : a.n;   // rows of the call
+  const int live = ROWS ? min(min(a.n_rows[blockIdx.y], a.max_rows), a.reqs[blockIdx.y].T) : a.n;   // rows of the call
   if (ROWS && n0 >= live) return;
   auto token = [&](int tb, int* pos) {   // token row of the workgroup's tb-th row, -1: none
     int64_t t = -1;
     if (n0 + tb < live) {
       if constexpr (ROWS) {
         const ReqDev rq = a.reqs[blockIdx.y];
-        t = (int64_t)rq.tok_off + a.rows[rq.tok_off + n0 + tb];
+        const int row = a.rows[rq.tok_off + n0 + tb];
+        if ((uint32_t)row >= (uint32_t)rq.T) return t;
+        t = (int64_t)rq.tok_off + row;
         *pos = a.tok_pos[t];
       } else {
         t = n0 + tb;

@@ -133,6 +133,11 @@ def qk_norm_rope_rows(plan: Plan, rows, n_rows, max_rows: int, q, k, gamma_q=Non
                       stream=None):
     """The same in place on the listed rows of a plan, at their positions in the new sequence (beside rope_rows)."""
     dt, d, at = _TYPES.get(plan.desc.dtype), plan.desc.head_dim, _device(q)
+    tokens = plan.info()["total_tokens"]
+    for t, heads, what in ((q, plan.desc.n_q_heads, "q"), (k, plan.desc.n_kv_heads, "k")):
+        _need(t.numel() == tokens * heads * d, f"{what} must be [{tokens}][{heads}][{d}], not {list(t.shape)}")
+    for t, n, what in ((rows, tokens, "rows"), (n_rows, plan.info()["n_requests"], "n_rows")):
+        _need(isinstance(t, int) or t.numel() >= n, f"{what} needs {n} entries")
     _check(lib().sx_qk_norm_rope_rows(plan.handle, rows if isinstance(rows, int) else _ptr(rows, _I32, at, "rows"),
                                       n_rows if isinstance(n_rows, int) else _ptr(n_rows, _I32, at, "n_rows"),
                                       int(max_rows), _ptr(q, dt, at, "q"), _ptr(k, dt, at, "k"),

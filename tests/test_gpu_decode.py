@@ -203,6 +203,19 @@ def test_qk_norm_rope_rows(dtype, d):
         first[[offs[r] + t for t in lists[r][:3]]] = True
     assert torch.equal(q2.cpu()[first], qd.cpu()[first]) and torch.equal(q2.cpu()[~first], q[~first])
     assert torch.equal(k2.cpu()[~first], k[~first])
+    # rows beyond their request, and counts beyond its length, are left out
+    bad, q3, k3 = rows.clone(), q.cuda(), k.cuda()
+    bad[offs[0] + 1], bad[offs[0] + 2], bad[offs[1] + 1] = -4, 292, 50
+    bad[offs[1] + 5:] = 1 << 30
+    sx.qk_norm_rope_rows(plan, bad.cuda(), i32([98, 1000]), 292, q3, k3, gq.cuda(), gk.cuda(), 1e-5)
+    good = live.clone()
+    good[[offs[0] + 3, offs[0] + 6, offs[1] + 7]] = False
+    for got, all_rows, src in ((q3, qd, q), (k3, kd, k)):
+        assert torch.equal(got.cpu()[good], all_rows.cpu()[good]) and torch.equal(got.cpu()[~good], src[~good])
+    with pytest.raises(ValueError, match="q must be"):
+        sx.qk_norm_rope_rows(plan, rows.cuda(), i32([98, 5]), 98, qd[1:].contiguous(), kd)
+    with pytest.raises(ValueError, match="rows needs"):
+        sx.qk_norm_rope_rows(plan, rows[1:].cuda(), i32([98, 5]), 98, qd, kd)
     plan.close()
 
 
