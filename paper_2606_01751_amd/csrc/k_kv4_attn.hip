@@ -49,7 +49,10 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part
   for (int i = 0; i < N; ++i) {
     uint32_t w[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(rest[2 * e], rest[2 * e + 1]);
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pack_bf16x2(rest[2 * e], rest[2 * e + 1]);
+      if (i + 1 < N) asm("" : "+v"(w[e]));   // (the halves are taken from here, not rounded once more)
+    }
     part[i] = as_bf16x8(w[0], w[1], w[2], w[3]);
 #pragma unroll
     for (int e = 0; e < 4 && i + 1 < N; ++e) {
@@ -139,7 +142,7 @@ struct Request {
     len = max(min(a.lens[r], a.max_keys), 0);
     rows = nq * a.G;
     off = len - nq;
-    split = kv4_split(rows, len, a.Hkv);
+    split = kv4_split(rows, len, a.Hkv, a.most16, a.most256);
   }
 };
 
@@ -228,18 +231,22 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
   constexpr int OP = D + 4;                   // LDS row pitch
   __shared__ __attribute__((aligned(16))) float so[NW][16][OP];
   __shared__ float sm[NW][16], sl[NW][16];
+  __shared__ bf16x8_t sq[MT][NC][NQ][64];     // the rows' operands, in lane order
   const int row0 = tile * 16 * MT;
   const int G = a.G;
-  const int tid = threadIdx.x, lane = tid & 63;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));               // (nothing derived from it is kept from one item to the next)
+  const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lg = lane >> 4;
-  int row[MT], lim[MT];                       // this lane's rows, and the last key each sees
+  int row[MT], token[MT], lim[MT];            // this lane's rows, their tokens, and the last key each sees
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     row[t] = min(row0 + 16 * t + (lane & 15), q.rows - 1);
-    lim[t] = q.off + row[t] / G;
+    token[t] = a.group.of(row[t]);
+    lim[t] = q.off + token[t];
   }
-  const int lim_min = q.off + row0 / G, lim_max = q.off + min(row0 + 16 * MT - 1, q.rows - 1) / G;
+  const int lim_min = q.off + a.group.of(row0), lim_max = q.off + a.group.of(min(row0 + 16 * MT - 1, q.rows - 1));
   const int k0 = c * q.split.keys;            // (c < n: below len)
   const int k1 = (int)min(min(k0 + (int64_t)q.split.keys, (int64_t)q.len), (int64_t)lim_max + 1);
   const int32_t* table = a.table + (int64_t)r * a.max_blocks;
@@ -266,23 +273,25 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
       pg[j].load(pool + max(id[j], 0) * block_bytes, lane);   // (a missing block: any bytes, dropped below)
     }
   };
-  if (steps > 0) fetch(0, page[0], page_id[0]);
+  fetch(0, page[0], page_id[0]);
 
-  bf16x8_t qf[MT][NC][NQ];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const T* src = (const T*)a.q + (int64_t)(q.q0 + row[t] / G) * a.q_ld + (h * G + row[t] % G) * D + lg * (D / 4);
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
+    const T* src = (const T*)a.q + (int64_t)(q.q0 + token[t]) * a.q_ld + (h * G + row[t] - token[t] * G) * D + lg * (D / 4);
+    for (int i = wave; i < NC; i += NW) {
+      bf16x8_t qf[NQ];
       if constexpr (NQ == 1) {
-        qf[t][i][0] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + i * 8));
+        qf[0] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + i * 8));
       } else {
         float x[8];
         load8(src + i * 8, x);
-        split_parts<NQ>(x, qf[t][i]);
+        split_parts<NQ>(x, qf);
       }
+#pragma unroll
+      for (int p = 0; p < NQ; ++p) sq[t][i][p][lane] = qf[p];
     }
   }
+  lds_barrier();
   f32x4_t o[MT][NU];
   float m[MT], l[MT];
 #pragma unroll
@@ -295,24 +304,27 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
 
   auto step = [&](int i, Page<D> (&pg)[2], const int (&id)[2], Page<D> (&next)[2], int (&next_id)[2]) __attribute__((always_inline)) {
     const int kb = k0 + 32 * (wave + NW * i);
-    if (i + 1 < steps) fetch(i + 1, next, next_id);
+    fetch(i + 1, next, next_id);
     if (kb + 32 > q.len || id[0] < 0 || id[1] < 0) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) pg[j].drop_values_from(id[j] < 0 ? 0 : q.len - kb - 16 * j, lane);
     }
     f32x4_t sc[MT][2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int t = 0; t < MT; ++t) sc[t][0] = sc[t][1] = (f32x4_t){0, 0, 0, 0};
+    int at = lane;
+    asm volatile("" : "+v"(at));               // (read again in every step: the registers go to more waves)
 #pragma unroll
-      for (int t = 0; t < MT; ++t) sc[t][j] = (f32x4_t){0, 0, 0, 0};
+    for (int n = 0; n < NC; ++n) {
+      const bf16x8_t k0f = pg[0].k_part(n), k1f = pg[1].k_part(n);
 #pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const bf16x8_t kf = pg[j].k_part(n);
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int p = NQ - 1; p >= 0; --p) sc[t][j] = mfma16(kf, qf[t][n][p], sc[t][j]);
-      }
+        for (int p = NQ - 1; p >= 0; --p) {
+          const bf16x8_t qf = sq[t][n][p][at];
+          sc[t][0] = mfma16(k0f, qf, sc[t][0]);
+          sc[t][1] = mfma16(k1f, qf, sc[t][1]);
+        }
     }
     const bool edge = kb + 31 > lim_min;       // some row does not see every key of the step
     bf16x8_t pf[MT][NP];
@@ -433,7 +445,8 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
     }
     if (q.split.n == 1) {
       const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-      const int64_t at = (int64_t)(q.q0 + orow / G) * a.Hq + h * G + orow % G;
+      const int otoken = a.group.of(orow);
+      const int64_t at = (int64_t)(q.q0 + otoken) * a.Hq + h * G + orow - otoken * G;
       T* dst = (T*)a.out + at * D + d0;
 #pragma unroll
       for (int e = 0; e < EPT; e += 2) {
@@ -456,19 +469,19 @@ __device__ __forceinline__ uint32_t few_tiles(const Request& q) {   // (0: the r
   return sizeof(T) == 2 && q.rows > kKv4FewRows ? 0u : (uint32_t)(q.rows + 16 * MT - 1) / (16 * MT);
 }
 
-// A workgroup for every possible item: x = KV head, tile, request, y = chunk.  Chunks slowest: workgroups beyond a
+// A workgroup for every possible item: x = KV head, y = tile, request, z = chunk.  Chunks slowest: workgroups beyond a
 // request's last chunk end at once, and between live ones they would put these on a few shader engines.
 template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 1) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
-  const int h = blockIdx.x % (uint32_t)a.Hkv, c = blockIdx.y;
-  const uint32_t idx = blockIdx.x / (uint32_t)a.Hkv, tile = idx % (uint32_t)tiles, r = idx / (uint32_t)tiles;
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 2) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+  const int h = blockIdx.x, c = blockIdx.z;
+  const uint32_t r = tiles > 1 ? blockIdx.y / (uint32_t)tiles : blockIdx.y, tile = blockIdx.y - r * tiles;
   const Request q(a, r);
   if (tile < few_tiles<T, MT>(q) && c < q.split.n) few_rows_item<T, D, MT, NW>(a, q, r, h, tile, c);
 }
 
 // Workgroups that take items in turn.
 template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void kv4_attn_items_kernel(Kv4AttnK ka) {
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 3 : 2) void kv4_attn_items_kernel(Kv4AttnK ka) {
   const int h = blockIdx.x % (uint32_t)ka.Hkv;
   for (uint32_t item = blockIdx.x / (uint32_t)ka.Hkv;; item += gridDim.x / (uint32_t)ka.Hkv) {
     const Kv4AttnK a = item_args();
@@ -522,10 +535,10 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
   const int wrow = row0 + wave * 32;
   const int row = min(wrow + l32, q.rows - 1);
   const bool valid = wrow + l32 < q.rows;
-  const int lim = q.off + row / G;
-  const int lim0 = q.off + row0 / G, lim1 = q.off + min(row0 + kWideCols - 1, q.rows - 1) / G;   // of the workgroup
-  const int wave_min = q.off + min(wrow, q.rows - 1) / G;
-  const int wave_max = wrow < q.rows ? q.off + min(wrow + 31, q.rows - 1) / G : -1;
+  const int token = a.group.of(row), lim = q.off + token;
+  const int lim0 = q.off + a.group.of(row0), lim1 = q.off + a.group.of(min(row0 + kWideCols - 1, q.rows - 1));   // of the workgroup
+  const int wave_min = q.off + a.group.of(min(wrow, q.rows - 1));
+  const int wave_max = wrow < q.rows ? q.off + a.group.of(min(wrow + 31, q.rows - 1)) : -1;
   const int k0 = c * q.split.keys;    // (a multiple of kKv4Step = 128)
   const int k1 = (int)min(min(k0 + (int64_t)q.split.keys, (int64_t)q.len), (int64_t)lim1 + 1);
   const int nkt = k1 > k0 ? (k1 - k0 + kWideKeys - 1) / kWideKeys : 0;
@@ -534,7 +547,7 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
 
   bf16x8_t qb[NS];
   {
-    const uint16_t* src = (const uint16_t*)a.q + (int64_t)(q.q0 + row / G) * a.q_ld + (h * G + row % G) * D + hg * 8;
+    const uint16_t* src = (const uint16_t*)a.q + (int64_t)(q.q0 + token) * a.q_ld + (h * G + row - token * G) * D + hg * 8;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qb[s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(src + s * 16));
   }
@@ -754,7 +767,7 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
   // columns (D / 16) cg + 2 dt + n of the lane: cg = 8 g + 4 hg + i, element e = 8 n + 4 g + i
   if (q.split.n == 1) {
     const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
-    const int64_t at = (int64_t)(q.q0 + row / G) * a.Hq + h * G + row % G;
+    const int64_t at = (int64_t)(q.q0 + token) * a.Hq + h * G + row - token * G;
     uint16_t* dst = (uint16_t*)a.out + at * D;
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -815,7 +828,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = FOUR ? blockIdx.y : blockIdx.y * 4 + wave;
   if (head >= a.Hq) return;
-  const int h = head / (uint32_t)a.G;
+  const int h = a.group.of(head);
   for (int token = blockIdx.x; token < a.total_q; token += gridDim.x) {
     const int r = __builtin_amdgcn_readfirstlane(lower_bound_wave(a.cu + 1, a.n_req, token + 1, lane));
     if (r >= a.n_req) return;                // behind the last sequence
@@ -826,7 +839,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
       continue;
     }
     if (i < 0 || i >= q.nq) continue;
-    const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + i * a.G + head % (uint32_t)a.G;
+    const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + i * a.G + head - h * a.G;
     const float2 ml = lane < n ? a.part_ml[at + (int64_t)lane * q.rows] : make_float2(kNegInf, 0.0f);   // n <= 64: a chunk per lane
     const float* src = a.part + at * D + lane * E;
     const float mt = wave_max(ml.x);
@@ -894,7 +907,7 @@ template <typename T, int D, int MT>
 static void launch_few(const Kv4AttnK& a, int64_t rows, int splits, hipStream_t s) {
   const int64_t tiles = (rows + 16 * MT - 1) / (16 * MT), all = tiles * a.Hkv * a.n_req;
   if (all * splits <= kDirectGroups) {
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4>), dim3((unsigned)all, (unsigned)splits), dim3(256), 0, s, a, (int)tiles);
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4>), dim3((unsigned)a.Hkv, (unsigned)(tiles * a.n_req), (unsigned)splits), dim3(256), 0, s, a, (int)tiles);
     return;
   }
   // at most so many tiles by the rows of q, too

@@ -366,6 +366,9 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   a.Hq = desc->n_q_heads;
   a.Hkv = desc->n_kv_heads;
   a.G = (int)G;
+  a.most16 = (int)sx::kv4_most_chunks(16, (uint32_t)a.Hkv);
+  a.most256 = (int)sx::kv4_most_chunks(256, (uint32_t)a.Hkv);
+  a.group = sx::kv4_heads((uint32_t)a.G);
   a.scale = (float)((double)sx::softmax_scale(desc) * 1.4426950408889634074);
   if (SX_DEVICE_CHECKS) {
     int v[4] = {0, 0, 0, 0};

@@ -30,18 +30,31 @@ constexpr int kKv4Step = 128;    // a chunk's length is a multiple of this
 struct Kv4Split {
   int n, keys;   // chunks, and keys of each but the last
 };
-__host__ __device__ inline uint32_t kv4_most_chunks(uint32_t rows, uint32_t heads) {
+inline uint32_t kv4_most_chunks(uint32_t rows, uint32_t heads) {
   const uint32_t counted = rows <= 16 ? 16 : rows <= 256 ? 256 : rows;
   const uint32_t n = kKv4Parts / counted / heads;
   return n < 1 ? 1 : n > kKv4Splits ? kKv4Splits : n;
 }
-__host__ __device__ inline Kv4Split kv4_split(int rows, int len, int heads) {   // (32-bit divisions: len <= 2^30)
-  const uint32_t most = kv4_most_chunks(rows, heads);
-  uint32_t n = ((uint32_t)len + kKv4Chunk - 1) / kKv4Chunk;
-  n = n < 1 ? 1 : n > most ? most : n;
-  const uint32_t keys = (((uint32_t)len + n - 1) / n + kKv4Step - 1) / kKv4Step * kKv4Step;
-  const uint32_t used = keys > 0 ? ((uint32_t)len + keys - 1) / keys : 1;
-  return {(int)(used < 1 ? 1 : used), (int)keys};
+// (most16, most256: kv4_most_chunks of up to 16 and 256 rows)
+__device__ inline Kv4Split kv4_split(int rows, int len, int heads, int most16, int most256) {
+  uint32_t most = rows <= 16 ? most16 : most256;
+  if (rows > 256) most = min(max(kKv4Parts / (uint32_t)rows / (uint32_t)heads, 1u), (uint32_t)kKv4Splits);
+  const uint32_t n = min(max(((uint32_t)len + kKv4Chunk - 1) / kKv4Chunk, 1u), most);
+  const uint32_t units = ((uint32_t)len + kKv4Step - 1) / kKv4Step & 0xffffff;   // (len <= 2^30: 24-bit divisions)
+  const uint32_t per = (units + n - 1) / n;
+  return {(int)(per > 0 ? (units + per - 1) / per : 1), (int)(per * kKv4Step)};
+}
+// Division by the heads of a group: n / G = n * magic >> (31 + shift) for 0 <= n < 2^31, with 2^shift the next power of
+// two and magic = 2^(31 + shift) / G + 1, which is too large by at most 1, so the product by less than 2^(31 + shift) / G.
+struct Kv4Heads {
+  uint32_t magic;
+  int shift;
+  __host__ __device__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * magic >> (31 + shift)); }
+};
+inline Kv4Heads kv4_heads(uint32_t g) {
+  int s = 0;
+  while ((1u << s) < g) ++s;
+  return {(uint32_t)(((uint64_t)1 << (31 + s)) / g + 1), s};
 }
 // most chunks, and most partial rows per head (rows x chunks, where there is more than one chunk), of a request of
 // at most `rows` rows and `len` keys
@@ -117,6 +130,8 @@ struct Kv4AttnK {
   float2* part_ml;      // [n_req][Hkv][part_rows] (max, sum), base-2 scores
   int64_t n_blocks, part_rows;
   int max_blocks, n_req, total_q, max_q, max_keys, Hq, Hkv, G;   // max_keys: min(max_seqlen, max_blocks * 16)
+  int most16, most256;  // kv4_split
+  Kv4Heads group;       // division by G
   float scale;          // softmax scale * log2(e)
 };
 hipError_t launch_kv4_attn(const Kv4AttnK& a, int D, bool f32, hipStream_t s);
