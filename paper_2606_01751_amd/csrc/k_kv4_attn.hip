@@ -69,19 +69,26 @@ template <int D>
 struct Page {
   uint32_t k[D / 32], v[D / 32];
   uint32_t ks, vs;
-  __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
-    const int tok = lane & 15, lg = lane >> 4;
+  // byte offsets in a record; kept apart from the record's address, which is uniform: a load takes both as they are
+  struct At {
+    uint32_t code, ks, vs;
+    __device__ __forceinline__ explicit At(uint32_t lane)
+        : code(lane * (D / 8)), ks(kv4_k_scales(D) + (lane >> 4) * (D / 4) / kKv4Group * 16 + (lane & 15)),
+          vs(kv4_v_scales(D) + (lane & 15) * (D / 16) / kKv4Group * 16 + 4 * (lane >> 4)) {}
+    __device__ __forceinline__ void here() { asm volatile("" : "+v"(code), "+v"(ks), "+v"(vs)); }
+  };
+  __device__ __forceinline__ void load(const uint8_t* rec, At at) {
     if constexpr (D == 128) {
-      const uint4 x = *(const uint4*)(rec + lane * 16), y = *(const uint4*)(rec + kv4_v_codes(D) + lane * 16);
+      const uint4 x = *(const uint4*)(rec + at.code), y = *(const uint4*)(rec + at.code + kv4_v_codes(D));
       k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
       v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
     } else {
-      const uint2 x = *(const uint2*)(rec + lane * 8), y = *(const uint2*)(rec + kv4_v_codes(D) + lane * 8);
+      const uint2 x = *(const uint2*)(rec + at.code), y = *(const uint2*)(rec + at.code + kv4_v_codes(D));
       k[0] = x.x; k[1] = x.y;
       v[0] = y.x; v[1] = y.y;
     }
-    ks = rec[kv4_k_scales(D) + lg * (D / 4) / kKv4Group * 16 + tok];
-    vs = *(const uint32_t*)(rec + kv4_v_scales(D) + tok * (D / 16) / kKv4Group * 16 + 4 * lg);
+    ks = rec[at.ks];
+    vs = *(const uint32_t*)(rec + at.vs);
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -265,12 +272,14 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
   // wait for its load.  (Two and three steps ahead were no faster: 36 us and 37.5 for one token over 131072 keys.)
   Page<D> page[2][2];
   int page_id[2][2];
+  typename Page<D>::At at(lane);
   auto fetch = [&](int i, Page<D> (&pg)[2], int (&id)[2]) __attribute__((always_inline)) {
     if (i > 0 && (i & 31) == 0) ids = load_ids(i >> 5);
+    at.here();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       id[j] = __builtin_amdgcn_readlane(ids, 2 * (i & 31) + j);
-      pg[j].load(pool + max(id[j], 0) * block_bytes, lane);   // (a missing block: any bytes, dropped below)
+      pg[j].load(pool + max(id[j], 0) * block_bytes, at);   // (a missing block: any bytes, dropped below)
     }
   };
   fetch(0, page[0], page_id[0]);
@@ -312,8 +321,8 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
     f32x4_t sc[MT][2];
 #pragma unroll
     for (int t = 0; t < MT; ++t) sc[t][0] = sc[t][1] = (f32x4_t){0, 0, 0, 0};
-    int at = lane;
-    asm volatile("" : "+v"(at));               // (read again in every step: the registers go to more waves)
+    int l64 = lane;
+    asm volatile("" : "+v"(l64));              // (read again in every step: the registers go to more waves)
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
       const bf16x8_t k0f = pg[0].k_part(n), k1f = pg[1].k_part(n);
@@ -321,7 +330,7 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
       for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int p = NQ - 1; p >= 0; --p) {
-          const bf16x8_t qf = sq[t][n][p][at];
+          const bf16x8_t qf = sq[t][n][p][l64];
           sc[t][0] = mfma16(k0f, qf, sc[t][0]);
           sc[t][1] = mfma16(k1f, qf, sc[t][1]);
         }
