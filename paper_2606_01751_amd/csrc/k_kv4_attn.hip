@@ -480,8 +480,8 @@ __device__ __forceinline__ uint32_t few_tiles(const Request& q) {   // (0: the r
 
 // A workgroup for every possible item: x = KV head, y = tile, request, z = chunk.  Chunks slowest: workgroups beyond a
 // request's last chunk end at once, and between live ones they would put these on a few shader engines.
-template <typename T, int D, int MT, int NW>
-__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? (MT == 1 ? 3 : 2) : 2) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
+template <typename T, int D, int MT, int NW, int WAVES>
+__global__ __launch_bounds__(NW * 64, WAVES) void kv4_attn_kernel(Kv4AttnK a, int tiles) {
   const int h = blockIdx.x, c = blockIdx.z;
   const uint32_t r = tiles > 1 ? blockIdx.y / (uint32_t)tiles : blockIdx.y, tile = blockIdx.y - r * tiles;
   const Request q(a, r);
@@ -907,6 +907,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
 // Workgroups of a launch.  64 requests of 1000 keys cost 15.6 us where the host says 1000 keys, but took 43 where it
 // says 131072 and every possible chunk had a workgroup, 305 with bounds of 512 queries beside it.
 constexpr int64_t kDirectGroups = 4096;   // most workgroups launched for possible items
+constexpr int64_t kWaves3Groups = 1024;   // workgroups from which three waves of two tiles a SIMD pay
 constexpr int64_t kFewGroups = 2048;      // ... that take items in turn: a few a compute unit
 constexpr int64_t kWideDirect = 2048;     // the same of the kernel for many rows, of which one fits a compute unit
 constexpr int64_t kWideGroups = 512;
@@ -916,7 +917,18 @@ template <typename T, int D, int MT>
 static void launch_few(const Kv4AttnK& a, int64_t rows, int splits, hipStream_t s) {
   const int64_t tiles = (rows + 16 * MT - 1) / (16 * MT), all = tiles * a.Hkv * a.n_req;
   if (all * splits <= kDirectGroups) {
-    hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4>), dim3((unsigned)a.Hkv, (unsigned)(tiles * a.n_req), (unsigned)splits), dim3(256), 0, s, a, (int)tiles);
+    // waves a SIMD.  Two tiles of d = 128 take 181 registers: three cost a few spills, which pays where there is work for
+    // them (64 requests of 16 tokens, 28 / 4 heads, over 4096 keys 151 us for 160), not in smaller launches (8 requests
+    // of 8192 keys 20.9 us for 20.4).
+    constexpr int W = sizeof(T) == 2 && MT == 1 ? 3 : 2;
+    const dim3 grid((unsigned)a.Hkv, (unsigned)(tiles * a.n_req), (unsigned)splits);
+    if constexpr (sizeof(T) == 2 && MT == 2 && D == 128) {
+      if (all * splits >= kWaves3Groups) {
+        hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4, 3>), grid, dim3(256), 0, s, a, (int)tiles);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((kv4_attn_kernel<T, D, MT, 4, W>), grid, dim3(256), 0, s, a, (int)tiles);
     return;
   }
   // at most so many tiles by the rows of q, too
