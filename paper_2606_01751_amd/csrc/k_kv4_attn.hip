@@ -20,8 +20,8 @@ namespace {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 constexpr float kNegInf = -__builtin_huge_valf();
 // Requests of more rows per KV head than this take the kernel for many rows (bfloat16).  Measured on both, few / many:
-// 80 rows over 16384 keys (2 requests of 8 heads) 38.5 / 53 us, 96 rows over 16384 (8 of 2) 36 / 55, 128 over 16384 (8
-// of 2) 43 / 58, 128 over 32768 (1 of 8) 46 / 44.
+// 80 rows over 16384 keys (2 requests of 8 heads) 36 / 40 us, 128 over 16384 (8 of 2) 43 / 44, 128 over 4096 (16 of 8)
+// 80 / 89, 160 over 8192 (4 of 8) 49 / 51, 192 over 32768 (1 of 8) 55 / 54, 256 over 32768 (1 of 8) 70 / 61.
 constexpr int kKv4FewRows = 128;
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -225,9 +225,11 @@ __device__ __forceinline__ void for_each(F&& f) {
 // two blocks in turn; the next step's codes are loaded while a step is computed, the block ids of 32 steps at
 // once.  Writes the rows' results, or their parts where the request's keys are split.  (Adding them up in the
 // workgroup that ends last saved nothing over the merge launch: 38.6 us for 34.6, 50.2 for 47.5 on the two cases
-// below.)  Bound by HBM where there is work for every compute unit: 64 requests of up to 8192 keys (28 / 4 heads, d =
-// 128) 47.5 us with the merge, 3.4 TB/s; 256 of 1024 keys (32 / 8) 58.8 us, 4.9 TB/s; one of 131072 keys 34.6 us, 4.1
-// TB/s; a plain streaming read reaches 5.5 - 6.
+// below.)  16 rows are bound by HBM where there is work for every compute unit: 64 requests of up to 8192 keys (28 / 4
+// heads, d = 128) 45.8 us with the merge, 3.5 TB/s; 256 of 1024 keys (32 / 8) 58 us, 5.0 TB/s; 256 of 8192 keys 468 us,
+// 5.0 TB/s; one of 131072 keys 34.7 us, 4.1 TB/s; a plain streaming read reaches 5.5 - 6.  32 rows are bound by the
+// vector ALU (two thirds of its cycles; conversions, exponentials and the parts of the probabilities): 128 requests of 5
+// tokens over 4608 keys (32 / 8 heads) 205 us, 3.1 TB/s.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D, int MT, int NW>
 __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& q, int r, int h, int tile, int c) {
@@ -269,7 +271,9 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
   };
   int ids = load_ids(0);
   // codes of the current and the next step: the loop below names the slots in turn, since a register copy would
-  // wait for its load.  (Two and three steps ahead were no faster: 36 us and 37.5 for one token over 131072 keys.)
+  // wait for its load.  Every step fetches, the last one block 0 (all its pages are missing): were the loads skipped
+  // on a path, each step would have to wait for all that are under way.  (Two steps ahead were no faster: 121 us
+  // for 121 for 64 requests of 8192 keys.)
   Page<D> page[2][2];
   int page_id[2][2];
   typename Page<D>::At at(lane);
@@ -521,7 +525,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 3 : 2) void kv4_attn_item
 // typical size, is that of its own rounding (0.0024 relative with both, 0.0017 with the output's alone), and two
 // parts cost 1378 us where one costs 964.  Sums and statistics are float32; the running maximum is raised only
 // when a probability would reach 2^24.
-// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 940 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
+// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 939 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
 // 1.26); the kernel for few rows took 11.4 ms.  Deeper operand reads (2 to 8 MFMAs ahead) change nothing, without its
 // softmax or its conversion the loop takes 970 and 837 us: bound by the matrix phase, whose MFMAs run at about that rate.
 // ---------------------------------------------------------------------------------------------
