@@ -9,7 +9,9 @@
 // are 16 consecutive bytes of a block; K's become so by a transposition over the four lanes of a group).  The
 // scale comes from the largest absolute value's bits: 2^E with 1.m >= 1.75 (m > 0x600000) needs e = E - 1, else
 // E - 2 (7 * 2^e = 1.75 * 2^(e + 2)).  The conversion instruction rounds to nearest with ties to even and
-// saturates, which is the definition; every 4-bit value is a bfloat16 value, so reading is exact.
+// saturates, which is the definition; every 4-bit value is a bfloat16 value, so reading is exact.  Both are bound by HBM:
+// 2048 blocks of 8 heads of 128 (bfloat16) take 34 us, 5.0 TB/s read and written, and back, the pool still in the cache,
+// 27.6 us, 6.2 TB/s.
 #include "sx_kv4_device.h"
 
 namespace sx {
@@ -48,8 +50,30 @@ __device__ __forceinline__ void quad_transpose(uint32_t (&x)[4], int m) {
   }
 }
 
+// Eight elements as they lie in memory: 4 or 8 dwords.  (Rows become float32 a group at a time: 52 registers, eight waves a
+// SIMD; all of them at once took 92, and 2048 blocks of 8 heads of 128 41 us instead of 34.)
+template <typename T>
+struct Raw8 {
+  uint32_t w[sizeof(T) * 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const uint4 v = ((const uint4*)p)[i];
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 2) return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+    else return __uint_as_float(w[e]);
+  }
+};
+
 // Eight elements -> codes and their group's scale byte.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t* byte) {
+template <typename T>
+__device__ __forceinline__ uint32_t quantise8(const Raw8<T>& raw, uint32_t* byte) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = raw.at(e);
   // as integers: the absolute values order like their bits, and NaN and infinity come out on top
   uint32_t top = 0;
 #pragma unroll
@@ -98,11 +122,11 @@ __device__ __forceinline__ bool locate(const Kv4MoveK& a, int tile, int t, int h
 template <typename T, int D, bool BLOCKS>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4MoveK a, int tiles) {
   constexpr int LPR = D / 8, NI = LPR / 4;   // lanes a row, steps
-  const uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (item >= (uint32_t)tiles * a.Hkv) return;
   const int tile = item / (uint32_t)a.Hkv, h = item % (uint32_t)a.Hkv;
   const int lane = threadIdx.x & 63, d = lane % LPR * 8, m = lane & 3;
-  float k[NI][8], v[NI][8];
+  Raw8<T> k[NI], v[NI];
   uint8_t* rec[NI];
   int tt[NI];
   bool live[NI];
@@ -113,16 +137,16 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4MoveK a, int tiles) {
     tt[i] = 0;
     if constexpr (!BLOCKS) {                 // (the rows are on their way beside the slots)
       const int64_t row = min(tile * kBlock + lane / LPR * NI + i, a.n - 1);
-      load8((const T*)a.k + row * a.k_ld + h * D + d, k[i]);
-      load8((const T*)a.v + row * a.v_ld + h * D + d, v[i]);
+      k[i].load((const T*)a.k + row * a.k_ld + h * D + d);
+      v[i].load((const T*)a.v + row * a.v_ld + h * D + d);
     }
     live[i] = locate<D, BLOCKS>(a, tile, lane / LPR * NI + i, h, &ko, &vo, &rec[i], &tt[i]);
-    if (BLOCKS && live[i]) {
-      load8((const T*)a.k + ko + d, k[i]);
-      load8((const T*)a.v + vo + d, v[i]);
+    if constexpr (BLOCKS) {
+      if (!live[0]) return;                  // (one block: all or none)
+      k[i].load((const T*)a.k + ko + d);
+      v[i].load((const T*)a.v + vo + d);
     }
   }
-  if (BLOCKS && !live[0]) return;            // (one block: all or none)
   uint32_t kw[NI] = {}, vw[NI] = {}, kb[NI] = {}, vb[NI] = {};
 #pragma unroll
   for (int i = 0; i < NI; ++i)
@@ -198,7 +222,7 @@ __device__ __forceinline__ void put8(T* p, uint32_t w, float s) {
 template <typename T, int D, bool BLOCKS>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4MoveK a, int tiles) {
   constexpr int LPR = D / 8, NI = LPR / 4;
-  const uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (item >= (uint32_t)tiles * a.Hkv) return;
   const int tile = item / (uint32_t)a.Hkv, h = item % (uint32_t)a.Hkv;
   const int lane = threadIdx.x & 63, d = lane % LPR * 8;
