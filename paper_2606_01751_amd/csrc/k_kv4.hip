@@ -50,24 +50,6 @@ __device__ __forceinline__ void quad_transpose(uint32_t (&x)[4], int m) {
   }
 }
 
-// Eight elements as they lie in memory: 4 or 8 dwords.  (Rows become float32 a group at a time: 52 registers, eight waves a
-// SIMD; all of them at once took 92, and 2048 blocks of 8 heads of 128 41 us instead of 34.)
-template <typename T>
-struct Raw8 {
-  uint32_t w[sizeof(T) * 2];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-      const uint4 v = ((const uint4*)p)[i];
-      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
-  }
-  __device__ __forceinline__ float at(int e) const {
-    if constexpr (sizeof(T) == 2) return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
-    else return __uint_as_float(w[e]);
-  }
-};
-
 // Eight elements -> codes and their group's scale byte.
 template <typename T>
 __device__ __forceinline__ uint32_t quantise8(const Raw8<T>& raw, uint32_t* byte) {
@@ -121,6 +103,8 @@ __device__ __forceinline__ bool locate(const Kv4MoveK& a, int tile, int t, int h
 
 template <typename T, int D, bool BLOCKS>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4MoveK a, int tiles) {
+  // (rows become float32 a group at a time: 52 registers, eight waves a SIMD; all of them at once took 92, and 2048
+  // blocks of 8 heads of 128 41 us instead of 34)
   constexpr int LPR = D / 8, NI = LPR / 4;   // lanes a row, steps
   const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (item >= (uint32_t)tiles * a.Hkv) return;

@@ -35,6 +35,23 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   }
 }
 
+// Eight elements as they lie in memory: 4 or 8 dwords.
+template <typename T>
+struct Raw8 {
+  uint32_t w[sizeof(T) * 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const uint4 v = ((const uint4*)p)[i];
+      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 2) return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+    else return __uint_as_float(w[e]);
+  }
+};
+
 // Four dwords of codes have eight elements each; a byte's two elements as bfloat16 times 2^e (s: float32 2^e,
 // NaN groups +inf: the instruction reads the exponent, 255 as NaN).  Exact for every byte and scale.
 template <int BYTE>
