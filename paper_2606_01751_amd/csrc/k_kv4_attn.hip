@@ -143,10 +143,11 @@ struct Page {
 struct Request {
   int q0, nq, len, rows, off;   // first query row, query tokens, keys, rows per KV head, position of the first query
   Kv4Split split;
-  __device__ __forceinline__ Request(const Kv4AttnK& a, int r) {
-    q0 = min(max(a.cu[r], 0), a.total_q);
-    nq = max(min(min(a.cu[r + 1], a.total_q) - q0, a.max_q), 0);
-    len = max(min(a.lens[r], a.max_keys), 0);
+  __device__ __forceinline__ Request(const Kv4AttnK& a, int r) : Request(a, a.cu[r], a.cu[r + 1], a.lens[r]) {}
+  __device__ __forceinline__ Request(const Kv4AttnK& a, int from, int to, int keys) {
+    q0 = min(max(from, 0), a.total_q);
+    nq = max(min(min(to, a.total_q) - q0, a.max_q), 0);
+    len = max(min(keys, a.max_keys), 0);
     rows = nq * a.G;
     off = len - nq;
     split = kv4_split(rows, len, a.Hkv, a.most16, a.most256);
@@ -843,9 +844,24 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   if (head >= a.Hq) return;
   const int h = a.group.of(head);
   for (int token = blockIdx.x; token < a.total_q; token += gridDim.x) {
-    const int r = __builtin_amdgcn_readfirstlane(lower_bound_wave(a.cu + 1, a.n_req, token + 1, lane));
-    if (r >= a.n_req) return;                // behind the last sequence
-    const Request q(a, r);
+    int r, q0, q1, keys;                   // the token's request
+    if (a.n_req <= 64) {                     // a lane each: one round of loads
+      q1 = lane < a.n_req ? a.cu[lane + 1] : INT32_MAX;
+      keys = lane < a.n_req ? a.lens[lane] : 0;
+      q0 = a.cu[0];
+      r = __popcll(__ballot(q1 <= token));
+      if (r >= a.n_req) return;              // behind the last sequence
+      if (r > 0) q0 = __builtin_amdgcn_readlane(q1, r - 1);
+      q1 = __builtin_amdgcn_readlane(q1, r);
+      keys = __builtin_amdgcn_readlane(keys, r);
+    } else {
+      r = __builtin_amdgcn_readfirstlane(lower_bound_wave(a.cu + 1, a.n_req, token + 1, lane));
+      if (r >= a.n_req) return;
+      q0 = a.cu[r];
+      q1 = a.cu[r + 1];
+      keys = a.lens[r];
+    }
+    const Request q(a, q0, q1, keys);
     const int i = token - q.q0, n = q.split.n;
     if (n == 1) {                            // on to the next request's tokens
       if (q.nq - i > (int)gridDim.x) token += (q.nq - i - 1) / gridDim.x * gridDim.x;
