@@ -832,12 +832,13 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK ka) {
   }
 }
 
-// The parts of split requests: a wave per (token, head), 32 chunks' loads in flight at once, or (FOUR) four waves, a
+// The parts of split requests: a wave per (token, head), up to 32 chunks' loads in flight at once (none for the
+// runs of 8 that there are no chunks for), or (FOUR) four waves, a
 // workgroup, with 16 each.  The chunks c, c + 4, .. are added in order, then the four sums, in both.
 template <typename T, int D, bool FOUR>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   constexpr int E = D / 64;                  // elements per lane
-  constexpr int STEP = FOUR ? 4 : 1, BATCH = FOUR ? kKv4Splits / 4 : 32;
+  constexpr int STEP = FOUR ? 4 : 1, BATCH = FOUR ? kKv4Splits / 4 : 32, RUN = FOUR ? BATCH : 8;
   __shared__ float so[FOUR ? 4 : 1][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = FOUR ? blockIdx.y : blockIdx.y * 4 + wave;
@@ -884,14 +885,22 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
     for (int c0 = FOUR ? wave : 0; c0 < n; c0 += BATCH * STEP) {
       float x[BATCH][E];
 #pragma unroll
-      for (int p = 0; p < BATCH; ++p)
+      for (int p0 = 0; p0 < BATCH; p0 += RUN) {
+        if (c0 + p0 * STEP >= n) break;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[p][e] = c0 + p * STEP < n ? src[(int64_t)(c0 + p * STEP) * q.rows * D + e] : 0.0f;
+        for (int p = p0; p < p0 + RUN; ++p)
 #pragma unroll
-      for (int p = 0; p < BATCH; ++p) {      // (behind the last chunk: f = 2^-inf = 0)
-        const float fc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), c0 + p * STEP));
+          for (int e = 0; e < E; ++e) x[p][e] = c0 + p * STEP < n ? src[(int64_t)(c0 + p * STEP) * q.rows * D + e] : 0.0f;
+      }
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[FOUR ? 0 : p & 3][e] = __builtin_fmaf(x[p][e], fc, acc[FOUR ? 0 : p & 3][e]);
+      for (int p0 = 0; p0 < BATCH; p0 += RUN) {
+        if (c0 + p0 * STEP >= n) break;
+#pragma unroll
+        for (int p = p0; p < p0 + RUN; ++p) {  // (behind the last chunk: f = 2^-inf = 0)
+          const float fc = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), c0 + p * STEP));
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[FOUR ? 0 : p & 3][e] = __builtin_fmaf(x[p][e], fc, acc[FOUR ? 0 : p & 3][e]);
+        }
       }
     }
     if constexpr (FOUR) {
