@@ -227,8 +227,8 @@ __device__ __forceinline__ void for_each(F&& f) {
 // once.  Writes the rows' results, or their parts where the request's keys are split.  (Adding them up in the
 // workgroup that ends last saved nothing over the merge launch: 38.6 us for 34.6, 50.2 for 47.5 on the two cases
 // below.)  16 rows are bound by HBM where there is work for every compute unit: 64 requests of up to 8192 keys (28 / 4
-// heads, d = 128) 45.8 us with the merge, 3.5 TB/s; 256 of 1024 keys (32 / 8) 58 us, 5.0 TB/s; 256 of 8192 keys 468 us,
-// 5.0 TB/s; one of 131072 keys 34.7 us, 4.1 TB/s; a plain streaming read reaches 5.5 - 6.  32 rows are bound by the
+// heads, d = 128) 44.6 us with the merge, 3.6 TB/s; 256 of 1024 keys (32 / 8) 58 us, 5.0 TB/s; 256 of 8192 keys 468 us,
+// 5.0 TB/s; one of 131072 keys 34.5 us, 4.1 TB/s; a plain streaming read reaches 5.5 - 6.  32 rows are bound by the
 // vector ALU (two thirds of its cycles; conversions, exponentials and the parts of the probabilities): 128 requests of 5
 // tokens over 4608 keys (32 / 8 heads) 205 us, 3.1 TB/s.
 // ---------------------------------------------------------------------------------------------
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 3 : 2) void kv4_attn_item
 // typical size, is that of its own rounding (0.0024 relative with both, 0.0017 with the output's alone), and two
 // parts cost 1378 us where one costs 964.  Sums and statistics are float32; the running maximum is raised only
 // when a probability would reach 2^24.
-// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 939 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
+// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 941 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
 // 1.26); the kernel for few rows took 11.4 ms.  Deeper operand reads (2 to 8 MFMAs ahead) change nothing, without its
 // softmax or its conversion the loop takes 970 and 837 us: bound by the matrix phase, whose MFMAs run at about that rate.
 // ---------------------------------------------------------------------------------------------
@@ -832,9 +832,9 @@ __global__ __launch_bounds__(512, 1) void kv4_attn_wide_kernel(Kv4AttnK ka) {
   }
 }
 
-// The parts of split requests: a wave per (token, head), up to 32 chunks' loads in flight at once (none for the
-// runs of 8 that there are no chunks for), or (FOUR) four waves, a
-// workgroup, with 16 each.  The chunks c, c + 4, .. are added in order, then the four sums, in both.
+// The parts of split requests: a wave per (token, head), up to 32 chunks' loads in flight at once (none for the runs of 8
+// that there are no chunks for), or (FOUR) four waves, a workgroup, with 16 each.  The chunks c, c + 4, .. are added in
+// order, then the four sums, in both.
 template <typename T, int D, bool FOUR>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnK a) {
   constexpr int E = D / 64;                  // elements per lane
