@@ -475,6 +475,41 @@ def test_kv4_attn_loose_bounds_and_many_requests(dtype):
         assert torch.equal(o, out[b.cu[r]:b.cu[r + 1]]), r
 
 
+@pytest.mark.parametrize("hq,hkv,nq", [(40, 8, 4), (30, 5, 6), (33, 11, 20), (26, 2, 9)])
+def test_kv4_attn_rows_of_large_launches(hq, hkv, nq):
+    # 17 to 128 rows a head, groups of 3, 5, 6 and 13: launches of more than 1024 workgroups, and each request by itself
+    g = torch.Generator().manual_seed(hq)
+    n = 1100 // (hkv * 3 * -(-nq * hq // hkv // 32)) + 2
+    sizes = [(nq - int(i % 3 == 2), int(k)) for i, k in enumerate(torch.randint(1500, 2500, (n,), generator=g))]
+    b = Batch(sizes, hq, hkv, 128, "bf16", seed=hkv)
+    out, _ = b.run(max_keys=2800)
+    q, kv = b.q[:nq].cpu(), [R.rows_of(b.pool.cpu(), b.table[0], b.nk[0], 128)]
+    want, _, bound, _ = R.attention(q, [0, nq], b.nk[:1], kv, 128 ** -0.5)
+    near(out[:nq], want, bound, "out bf16")
+    for r in (0, 2, n // 2, n - 1):
+        o = torch.empty_like(b.q[b.cu[r]:b.cu[r + 1]])
+        k = sizes[r][1]
+        ws = torch.empty(sx.kv4_attn_workspace(b.desc, 1, sizes[r][0], k), dtype=torch.uint8, device="cuda")
+        sx.kv4_attn(b.desc, b.q[b.cu[r]:b.cu[r + 1]].contiguous(), i32([0, sizes[r][0]]), i32([k]), b.table[r:r + 1].cuda().contiguous(),
+                    b.pool, o, sizes[r][0], k, ws)
+        assert torch.equal(o, out[b.cu[r]:b.cu[r + 1]]), r
+
+
+@pytest.mark.parametrize("dtype,nq", [("bf16", 1), ("bf16", 70), ("f32", 3)])
+def test_kv4_attn_large_values_and_rising_scores(dtype, nq):
+    # values of 2^70 under weights that stay below 2^24 before the division, scores that rise from key to key
+    b = Batch([(nq, 1500), (1, 40)], 4, 2, 64, dtype, seed=21)
+    for r, n in enumerate(b.nk):
+        t = torch.arange(n)
+        s = i32(b.table[r, t // 16] * 16 + t % 16)
+        k = (0.05 * t[:, None, None] * torch.ones(n, 2, 64)).cuda()
+        v = (2.0 ** 70 * torch.randn(n, 2, 64, generator=torch.Generator().manual_seed(r))).cuda()
+        sx.kv4_write(sx.make_desc(2, 2, 64, "f32", 1e4), k, v, s, b.pool)
+    b.q[:] = b.q * 0.01 + 0.02
+    out, _ = b.check()
+    assert torch.isfinite(out[:b.cu[-1]]).all() and out[:b.cu[-1]].abs().max() > 2.0 ** 60
+
+
 def test_kv4_attn_scale_and_empty_table():
     b = Batch([(3, 70), (1, 20)], 4, 2, 64, "f32", seed=1)
     b.desc = sx.make_desc(4, 2, 64, "f32", 1e4, softmax_scale=0.3)
