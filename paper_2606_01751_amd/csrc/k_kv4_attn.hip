@@ -353,7 +353,8 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
           if (id[e >> 2] < 0 || kb + 16 * (e >> 2) + 4 * lg + (e & 3) > lim[t]) s[e] = kNegInf;
       }
       // the maximum is raised only when a probability would reach 2^24 (or is not a number): the same softmax,
-      // and no maximum over the lanes in most steps
+      // and no maximum over the lanes in most steps.  Only for the rows that need it: another row's keys, which this one
+      // may not see, leave its bits alone
       float p[8], psum;
       auto expo = [&](float neg) {
         psum = 0.0f;
@@ -364,14 +365,15 @@ __device__ __forceinline__ void few_rows_item(const Kv4AttnK& a, const Request& 
         }
       };
       expo(-m[t]);
-      if (__any(!(psum < 0x1p24f))) {
+      if (const uint64_t high = __ballot(!(psum < 0x1p24f))) {
+        const bool raise = high >> (lane & 15) & 0x0001000100010001;   // (any of the row's four lanes)
         float top = s[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mn = fmaxf(m[t], top * a.scale);
-        const float f = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
+        const float mn = raise ? fmaxf(m[t], top * a.scale) : m[t];
+        const float f = !raise || mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
         l[t] *= f;
 #pragma unroll
         for (int u = 0; u < NU; ++u) o[t][u] *= f;
@@ -707,15 +709,16 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
       }
     };
     expo(-m_run);
-    if (__ballot(!(psum < 0x1p24f))) {
+    if (const uint64_t high = __ballot(!(psum < 0x1p24f))) {
+      const bool raise = high >> l32 & 0x100000001;   // (for the columns that need it, either of whose lanes says so)
       float mx = sacc[0][0];
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sacc[mt][e]);
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float m_new = fmaxf(m_run, mx * c2);
-      const float f = m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+      const float m_new = raise ? fmaxf(m_run, mx * c2) : m_run;
+      const float f = !raise || m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
@@ -946,7 +949,7 @@ template <typename T, int D, int MT>
 static void launch_few(const Kv4AttnK& a, int64_t rows, int splits, hipStream_t s) {
   const int64_t tiles = (rows + 16 * MT - 1) / (16 * MT), all = tiles * a.Hkv * a.n_req;
   if (all * splits <= kDirectGroups) {
-    // waves a SIMD.  Two tiles of d = 128 take 181 registers: three cost a few spills, which pays where there is work for
+    // waves a SIMD.  Two tiles of d = 128 take 183 registers: three cost a few spills, which pays where there is work for
     // them (64 requests of 16 tokens, 28 / 4 heads, over 4096 keys 151 us for 160), not in smaller launches (8 requests
     // of 8192 keys 20.9 us for 20.4).
     constexpr int W = sizeof(T) == 2 && MT == 1 ? 3 : 2;
