@@ -142,8 +142,9 @@ sx_status sx_kv4_attn_workspace(const sx_layer_desc* desc, int32_t n_requests, i
  *   time need one each.
  * Products run on the bfloat16 matrix cores with float32 accumulation: the 4-bit values are bfloat16
  * values, a float32 q and its probabilities go through as three bfloat16 parts, a bfloat16 call's
- * probabilities as two (requests of at most 128 rows, query tokens x heads of the group) or one.  Sums are
- * float32 and divided at the end, with weights below 2^24 in between: they hold for values up to 2^72. */
+ * probabilities as two (requests of at most 128 rows, query tokens x heads of the group) or one, divided by the
+ * sum of what was multiplied.  Sums are float32 and divided at the end, with weights below 2^24 in between: they
+ * hold for values up to 2^72. */
 sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, const int32_t* cu_q,
                       const int32_t* seq_lens, const int32_t* block_table, int32_t max_blocks, int32_t n_requests,
                       int32_t total_q, int32_t max_q, int32_t max_seqlen, const void* pool, int64_t n_blocks, void* out,

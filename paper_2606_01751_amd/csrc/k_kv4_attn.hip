@@ -38,6 +38,11 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The two bfloat16 values of w added to c.
+__device__ __forceinline__ float sum_bf16x2(uint32_t w, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), (bf16x2_t){1.0f, 1.0f}, c, false);
+}
+
 // A float32 as a sum of N bfloat16 parts, each the rounding of what the others leave: part i of x[0..8).  FINITE:
 // no infinities among them (otherwise one stands in the first part alone).
 template <int N, bool FINITE = false>
@@ -526,9 +531,12 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 3 : 2) void kv4_attn_item
 // write of T comes in iteration T - 1.
 // Probabilities are rounded to bfloat16 once, as in full and sparse attention: the error of a result, 2^-9 of its
 // typical size, is that of its own rounding (0.0024 relative with both, 0.0017 with the output's alone), and two
-// parts cost 1378 us where one costs 964.  Sums and statistics are float32; the running maximum is raised only
-// when a probability would reach 2^24.
-// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 941 us, 1.13 PFLOP/s (a plain 8192^3 bfloat16 product reaches
+// parts cost 1378 us where one costs 964.  A row is divided by the sum of the rounded probabilities, so a rounding
+// moves its result by 2^-8 w |v - result| at the most, w the key's weight, and nothing where one key has all of it (divided
+// by the exact sum: 2^-8 |v|); the exact sum, for the lse and the weights of parts, is kept beside it.  That costs 3 %
+// (945 us to 972; 979 with the sum formed in the vector phase).  Sums and statistics are float32; the running maximum is
+// raised only when a probability would reach 2^24.
+// 2048 tokens of 32 / 8 heads over 32768 keys (d = 128): 970 us, 1.10 PFLOP/s (a plain 8192^3 bfloat16 product reaches
 // 1.26); the kernel for few rows took 11.4 ms.  Deeper operand reads (2 to 8 MFMAs ahead) change nothing, without its
 // softmax or its conversion the loop takes 970 and 837 us: bound by the matrix phase, whose MFMAs run at about that rate.
 // ---------------------------------------------------------------------------------------------
@@ -572,7 +580,7 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
-  float m_run = kNegInf, l_run = 0.0f;
+  float m_run = kNegInf, l_run = 0.0f, r_run = 0.0f;   // maximum; sum of the probabilities, and of their roundings
 
   // ---- staging: this wave's block and matrix of every tile ----
   const int grp = wave >> 2;
@@ -678,6 +686,10 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8_t*)(vb + (kk * ND + dt) * 1024 + lane * 16), pb[kk],
                                                         o[dt], 0, 0, 0);
     sched_pipelined<4 * ND, 1, 4>();
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) r_run = sum_bf16x2(__builtin_bit_cast(u32x4_t, pb[kk])[t], r_run);
   };
   auto softmax_tile = [&](int j, int buf) {
     const int kbase = k0 + j * kWideKeys;
@@ -720,6 +732,7 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
       const float m_new = raise ? fmaxf(m_run, mx * c2) : m_run;
       const float f = !raise || m_new == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= f;
+      r_run *= f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
       m_run = m_new;
@@ -779,11 +792,11 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
   }
   if (!grp) lds_barrier();
 
-  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64), r_tot = r_run + __shfl_xor(r_run, 32, 64);
   if (!valid) return;
   // columns (D / 16) cg + 2 dt + n of the lane: cg = 8 g + 4 hg + i, element e = 8 n + 4 g + i
   if (q.split.n == 1) {
-    const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+    const float inv = l_tot == 0.0f ? 0.0f : 1.0f / r_tot;
     const int64_t at = (int64_t)(q.q0 + token) * a.Hq + h * G + row - token * G;
     uint16_t* dst = (uint16_t*)a.out + at * D;
 #pragma unroll
@@ -801,13 +814,14 @@ __device__ __forceinline__ void many_rows_item(const Kv4AttnK& a, const Request&
   } else {
     const int64_t at = ((int64_t)r * a.Hkv + h) * a.part_rows + (int64_t)c * q.rows + row;
     float* dst = a.part + at * D;
+    const float f = l_tot == 0.0f ? 0.0f : l_tot / r_tot;   // (the merge divides by the sum of all l)
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
-          *(float2*)(dst + (8 * g + 4 * hg + i) * (D / 16) + 2 * dt) = make_float2(o[dt][4 * g + i], o[dt][8 + 4 * g + i]);
+          *(float2*)(dst + (8 * g + 4 * hg + i) * (D / 16) + 2 * dt) = make_float2(o[dt][4 * g + i] * f, o[dt][8 + 4 * g + i] * f);
     if (hg == 0) a.part_ml[at] = make_float2(m_run, l_tot);
   }
 }

@@ -46,3 +46,47 @@ def test_a_key_behind_a_row_leaves_its_bits(hq, hkv, d, dtype, nq, nk, first, wh
         assert out2[first:nq].isnan().all() and lse2[first:nq].isnan().all()
     else:
         assert not torch.equal(out2[first:nq], out[first:nq]) and torch.isfinite(out2).all()
+
+
+def one_part_reference(b, r, extra=0.0):
+    """(out, bound) in float64 of request r of more than 128 rows in bfloat16.  A probability p_j goes into the product as
+    p_j (1 + e_j), |e_j| <= 2^-8, and the row is divided by the sum of these: off by at most 2^-8 sum w_j |v_j - out| over the
+    softmax weights w (times 1 + 2^-7 for the divisor's own error).  The float32 arithmetic as in kv4ref.attention, without
+    parts of a probability; `extra` on top of the relative error of a score."""
+    import kv4ref as R
+    q0, n, m, grp = b.cu[r], b.nq[r], b.nk[r], b.hq // b.hkv
+    k, v, ok = (x.cuda() for x in R.rows_of(b.pool.cpu(), b.table[r], m, b.d))
+    see = (torch.arange(m, device="cuda")[None] <= torch.arange(m - n, m, device="cuda")[:, None]) & ok[None]
+    out = torch.zeros(n, b.hq, b.d, dtype=torch.float64, device="cuda")
+    bound = torch.zeros_like(out)
+    scale = b.d ** -0.5
+    for h in range(b.hq):
+        kh, vh, qh = k[:, h // grp], v[:, h // grp], b.q[q0:q0 + n, h].double()
+        s = (qh @ kh.t().contiguous() * scale).masked_fill(~see, -math.inf)
+        w = s.softmax(-1)
+        out[:, h] = w @ vh
+        mag = (qh.abs() @ kh.abs().t().contiguous()).masked_fill(~see, 0).amax(-1) * scale
+        ds = mag * (b.d + 4) * 2.0 ** -24 + 2.0 ** -22 * (s.abs().masked_fill(~see, 0).amax(-1) + 1) + extra
+        fine = 2 * (ds + m * 2.0 ** -24 + 2.0 ** -22)[:, None] * (w @ vh.abs())
+        for i in range(n):
+            bound[i, h] = fine[i] + 2.0 ** -8 * (1 + 2.0 ** -7) * (w[i] @ (vh - out[i, h]).abs())
+    return out, bound
+
+
+@pytest.mark.parametrize("d,nq,nk", [(128, 150, 700), (64, 290, 290), (128, 200, 3000), (64, 140, 9000)])
+@pytest.mark.parametrize("peak", [0.0, 7.0, 12.0])
+def test_many_rows_divide_by_the_probabilities_that_were_multiplied(d, nq, nk, peak):
+    # peak: one key early in the second tile whose score lies that many nats above the first tile's, below the raise of the
+    # maximum: nearly all the weight of a row is on it, and the row's result is its value, whatever its probability's rounding
+    b = Batch([(nq, nk), (1, 33)], 2, 1, d, "bf16", seed=nq)
+    if peak:
+        g = torch.Generator().manual_seed(d)
+        unit = torch.ones(1, 1, d) / d ** 0.5                # scores in nats: q = a * ones, k = c * ones
+        put(b, 0, range(nk), 0.02 * torch.randn(nk, 1, d, generator=g), torch.randn(nk, 1, d, generator=g))
+        put(b, 0, [64], d ** 0.5 * unit, 1.5 * torch.sign(torch.randn(1, 1, d, generator=g)))
+        b.q[:nq] = (peak / d ** 0.5 * (1 + 0.2 * torch.rand(nq, 2, 1, generator=g))).expand(nq, 2, d).to(b.q.dtype).cuda()
+    out, _ = b.run()
+    want, bound = one_part_reference(b, 0)
+    eps = torch.finfo(torch.bfloat16).eps
+    off = (out[:nq].double() - want).abs() - (bound + eps / 2 * (want.abs() + bound))
+    assert off.max().item() <= 0, off.max().item()
