@@ -61,7 +61,8 @@ extern "C" {
  *   cu_new       [n_requests + 1] prefix sums of the new tokens: the rows of request r's new tokens
  *   positions    [max_tokens] token index of every new token in its request; -1 behind the last one
  *   slots        [max_tokens] block * block_size + offset; -1 behind the last one, and for a token
- *                that has no block (list used up, table too narrow, a negative table entry)
+ *                that has no block (list used up, table too narrow, a negative entry of table or list)
+ *                or whose slot int32 does not hold
  *   state        [2] the free list's next entry, and the number of new tokens that got no slot (0: all
  *                is well; tokens that do not fit into max_tokens count, their blocks are taken and entered
  *                in block_table all the same)
