@@ -81,8 +81,8 @@ sx_status sx_append_slots(const int32_t* ctx_lens, const int32_t* new_lens, int3
  * in float32 with one rounding at the end; angle and cos / sin in float64, rounded to float32.
  * positions [n_tokens] int32: a row with a negative position is neither computed nor written.
  * Rows are contiguous, ld elements apart (a multiple of 8, at least heads * d: the parts of a stacked
- * projection).  q_out, k_out may be q, k themselves with the same ld; they must not overlap them
- * otherwise.  Tensors are 16-byte aligned. */
+ * projection).  q_out, k_out may be q, k themselves with the same ld; otherwise their rows must not overlap
+ * each other or another argument (SX_EINVAL).  Tensors are 16-byte aligned. */
 sx_status sx_qk_norm_rope(const sx_layer_desc* desc, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
                           const void* gamma_q, const void* gamma_k, float eps, const int32_t* positions,
                           int32_t n_tokens, void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld,
@@ -91,7 +91,7 @@ sx_status sx_qk_norm_rope(const sx_layer_desc* desc, const void* q, int64_t q_ld
 /* The same for the listed rows of a plan, in place, each at its position in the new sequence
  * (new_pos of its segment + offset), as sx_rope_rows does without the norm: q [sum T][Hq][d],
  * k [sum T][Hkv][d], addressed by token; rows not listed are left alone, listed rows beyond their request
- * left out.  float32 and bfloat16. */
+ * left out.  q and k must not overlap each other or another argument.  float32 and bfloat16. */
 sx_status sx_qk_norm_rope_rows(const sx_plan* plan, const int32_t* rows, const int32_t* n_rows, int32_t max_rows,
                                void* q, void* k, const void* gamma_q, const void* gamma_k, float eps, void* stream);
 

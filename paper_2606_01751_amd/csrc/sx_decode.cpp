@@ -25,6 +25,36 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return a && b && na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// n rows of `width` bytes, `ld` bytes apart.
+struct Rows {
+  const void* p;
+  int64_t n, width, ld;
+};
+Rows whole(const void* p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+
+// Whether some row of x and some row of y have a byte in common.
+bool rows_overlap(Rows x, Rows y) {
+  typedef __int128 wide;
+  if (!x.p || !y.p || x.n <= 0 || y.n <= 0 || x.width <= 0 || y.width <= 0) return false;
+  for (Rows* r : {&x, &y})
+    if (r->n > 1 && r->ld == r->width && r->n <= INT64_MAX / r->ld) *r = whole(r->p, r->n * r->ld);   // contiguous: one row
+  const wide d = (wide)(uintptr_t)y.p - (wide)(uintptr_t)x.p;   // from x's first row to y's
+  if (d >= (wide)(x.n - 1) * x.ld + x.width || -d >= (wide)(y.n - 1) * y.ld + y.width) return false;
+  if (x.n == 1) x.ld = y.ld;
+  if (y.n == 1) y.ld = x.ld;
+  if (x.ld == y.ld) {
+    // row j of y begins at d + k ld of row i of x, k = j - i: the first k whose row ends behind x's begin decides
+    const wide t = -d - y.width;
+    const wide below = t >= 0 ? t / x.ld : -((-t + x.ld - 1) / x.ld);   // floor(t / ld)
+    const wide k = std::max<wide>(below + 1, -(wide)(x.n - 1));
+    return k < y.n && d + k * x.ld < x.width;
+  }
+  if (x.n > y.n) std::swap(x, y);
+  for (int64_t i = 0; i < x.n; ++i)
+    if (rows_overlap({(const char*)x.p + i * x.ld, 1, x.width, x.width}, y)) return true;
+  return false;
+}
+
 int esize(const sx_layer_desc* d) { return d->dtype == SX_F32 ? 4 : 2; }
 
 // Rows of `heads` heads each, ld elements apart.
@@ -220,6 +250,15 @@ sx_status sx_qk_norm_rope(const sx_layer_desc* desc, const void* q, int64_t q_ld
   if (!positions) return reportf(SX_EINVAL, "positions is NULL");
   if ((q_out == q && q_out_ld != q_ld) || (k_out == k && k_out_ld != k_ld))
     return reportf(SX_EINVAL, "in place, the rows must be as far apart in the output as in the input");
+  const int64_t es = esize(desc), head = desc->head_dim * es;
+  const Rows in[] = {{q, n_tokens, desc->n_q_heads * head, q_ld * es}, {k, n_tokens, desc->n_kv_heads * head, k_ld * es},
+                     whole(gamma_q, head), whole(gamma_k, head), whole(positions, 4ll * n_tokens)};
+  const Rows to[] = {{q_out, n_tokens, in[0].width, q_out_ld * es}, {k_out, n_tokens, in[1].width, k_out_ld * es}};
+  if (rows_overlap(to[0], to[1])) return reportf(SX_EINVAL, "q_out and k_out overlap");
+  for (int o = 0; o < 2; ++o)
+    for (int i = 0; i < 5; ++i)
+      if (!(i == o && to[o].p == in[i].p) && rows_overlap(to[o], in[i]))
+        return reportf(SX_EINVAL, "%s overlaps another argument (it may be %s itself)", o ? "k_out" : "q_out", o ? "k" : "q");
   sx::QkNormRopeK a{};
   a.q = q;
   a.k = k;
@@ -256,6 +295,12 @@ sx_status sx_qk_norm_rope_rows(const sx_plan* p, const int32_t* rows, const int3
   if (max_rows == 0) return SX_OK;
   if ((st = sx::check_row_list(p, rows, n_rows, max_rows, stream, "sx_qk_norm_rope_rows")) != SX_OK) return st;
   const sx_layer_desc& d = p->desc;
+  const int64_t head = d.head_dim * esize(&d);
+  const Rows arr[] = {whole(q, p->total * d.n_q_heads * head), whole(k, p->total * d.n_kv_heads * head), whole(gamma_q, head),
+                      whole(gamma_k, head), whole(rows, 4 * p->total), whole(n_rows, 4ll * p->n_req)};
+  for (int o = 0; o < 2; ++o)
+    for (int i = o + 1; i < 6; ++i)
+      if (rows_overlap(arr[o], arr[i])) return reportf(SX_EINVAL, "%s overlaps another argument", o ? "k" : "q");
   sx::QkNormRopeK a{};
   a.q = a.qo = q;
   a.k = a.ko = k;

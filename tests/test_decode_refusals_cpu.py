@@ -1,0 +1,43 @@
+"""Refusals of the decoding calls without a GPU, beside test_decode_cpu.py: arguments that overlap, and sizes that the C types
+do not hold."""
+import ctypes
+
+import pytest
+
+import paper_2606_01751_amd as sx
+from test_decode_cpu import A, desc, err, qk_args
+
+
+def qk(status=sx.SX_EINVAL, text="overlap", dtype="bf16", **kw):
+    err(sx.lib().sx_qk_norm_rope(ctypes.byref(desc(dtype=dtype)), *qk_args(**kw)), status, text)
+
+
+# bf16, 8 / 2 heads of 128: a row of q has 2048 bytes, a row of k 512; a qkv row 3072
+@pytest.mark.parametrize("kw", [
+    dict(qo=A + 2048), dict(qo=A + 4096 + 2032), dict(qo=A - 4096 - 2032), dict(qo=A + 0x10000), dict(qo=A + 0x10000 + 1520),
+    dict(qo=A + 0x20000), dict(qo=A + 0x21000 - 6128), dict(qo=A + 0x22000), dict(ko=A), dict(ko=A + 6128), dict(ko=A + 0x10200),
+    dict(ko=A + 0x30000 + 2048), dict(ko=A + 0x21000), dict(ko=A + 0x22000 - 16),
+    # parts of stacked rows, 1536 elements apart: one row behind, the part of q, one head into the other's part
+    dict(qld=1536, kld=1536, k=A + 2048, qo=A + 3072, qold=1536), dict(qld=1536, kld=1536, k=A + 2048, ko=A + 1536, kold=1536),
+    dict(qld=1536, kld=1536, k=A + 2048, qo=A, qold=1536, ko=A + 2048 + 256, kold=1536),
+    # rows of different distances
+    dict(qld=1536, qo=A + 3072 + 1024, qold=1544), dict(qld=1536, kld=256, k=A + 2048, ko=A + 2560, kold=2048),
+])
+def test_qk_norm_rope_refuses_overlapping_rows(kw):
+    qk(**kw)
+
+
+def _rows_meet(x, y):
+    return any(a < d and c < b for a, b in x for c, d in y)
+
+
+def test_overlap_is_that_of_the_rows():
+    # every offset of a short k_out over the rows of q: refused where a row meets a row, else the call goes on to its next
+    # check (eps, which comes before, is valid; a negative position pointer is not there to be read: n_tokens rows only)
+    for qld, kold, n in ((1536, 1536, 3), (1536, 256, 3), (1024, 1536, 2), (2048, 1536, 3), (1536, 1544, 4)):
+        q = [(A + i * qld * 2, A + i * qld * 2 + 2048) for i in range(n)]
+        for off in range(-4096, 3 * n * 4096, 1008):
+            at = A + off // 16 * 16
+            ko = [(at + i * kold * 2, at + i * kold * 2 + 512) for i in range(n)]
+            if _rows_meet(q, ko):
+                qk(qld=qld, ko=at, kold=kold, n=n, k=A + (1 << 24), gq=None, gk=None, pos=A + (1 << 25), qo=A + (1 << 26))
