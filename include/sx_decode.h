@@ -138,7 +138,8 @@ sx_status sx_kv4_attn_workspace(const sx_layer_desc* desc, int32_t n_requests, i
  *   cu_q [n_requests + 1], seq_lens [n_requests], block_table [n_requests][max_blocks]: DEVICE int32
  *   max_q, max_seqlen: host bounds of every n_r and seq_lens[r] (they size the launch; a request is cut
  *   to them); rows of q and out from cu_q[n_requests] on are left as they were
- *   out [total_q][Hq][d], lse [total_q][Hq] float32
+ *   out [total_q][Hq][d], lse [total_q][Hq] float32.  out may be q itself (q_ld = Hq * d); otherwise out, lse and
+ *   workspace must not overlap each other or another argument (SX_EINVAL)
  *   workspace: sx_kv4_attn_workspace bytes, 16-byte aligned, any content; calls in flight at the same
  *   time need one each.
  * Products run on the bfloat16 matrix cores with float32 accumulation: the 4-bit values are bfloat16

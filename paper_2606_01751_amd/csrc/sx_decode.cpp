@@ -390,6 +390,17 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
   if (workspace_bytes < need)
     return reportf(SX_ESHAPE, "sx_kv4_attn needs %lld bytes of workspace, got %lld", (long long)need, (long long)workspace_bytes);
   if (!aligned16(workspace)) return reportf(SX_EINVAL, "workspace is not 16-byte aligned");
+  // (a workgroup reads the rows of q that it writes before it writes them, and no other reads them: out may be q)
+  const int64_t es = esize(desc), width = desc->n_q_heads * desc->head_dim * es;
+  const Rows arr[] = {whole(out, total_q * width), whole(lse, 4ll * total_q * desc->n_q_heads), whole(workspace, need),
+                      {q, total_q, width, q_ld * es}, whole(cu_q, 4ll * (n_requests + 1ll)), whole(seq_lens, 4ll * n_requests),
+                      whole(block_table, 4ll * n_requests * max_blocks),
+                      whole(pool, n_blocks * desc->n_kv_heads * sx::kv4_record(desc->head_dim))};
+  const char* const names[] = {"out", "lse", "workspace"};
+  for (int o = 0; o < 3; ++o)
+    for (int i = o + 1; i < 8; ++i)
+      if (!(o == 0 && i == 3 && out == q && q_ld * es == width) && rows_overlap(arr[o], arr[i]))
+        return reportf(SX_EINVAL, "sx_kv4_attn: %s overlaps another argument (out may be q itself, with contiguous rows)", names[o]);
   sx::Kv4AttnK a{};
   a.q = q;
   a.q_ld = q_ld;

@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 import paper_2606_01751_amd as sx
-from test_decode_cpu import A, desc, err, qk_args
+from test_decode_cpu import A, attn_args, desc, err, qk_args
 
 
 def qk(status=sx.SX_EINVAL, text="overlap", dtype="bf16", **kw):
@@ -41,3 +41,20 @@ def test_overlap_is_that_of_the_rows():
             ko = [(at + i * kold * 2, at + i * kold * 2 + 512) for i in range(n)]
             if _rows_meet(q, ko):
                 qk(qld=qld, ko=at, kold=kold, n=n, k=A + (1 << 24), gq=None, gk=None, pos=A + (1 << 25), qo=A + (1 << 26))
+
+
+def attn(**kw):
+    # 2 rows of 2048 bytes, 4 blocks of 2 x 2176 bytes, up to 131072 keys; nothing overlaps unless kw says so
+    a = dict(q=A, out=A + 0x30000, pool=A + (1 << 24), nb=4, ws=A + (1 << 28), lse=A + 0x50000)
+    a.update(kw)
+    err(sx.lib().sx_kv4_attn(ctypes.byref(desc()), *attn_args(**a)), sx.SX_EINVAL, "overlap")
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=A + 2048), dict(out=A - 2048 - 16), dict(out=A, qld=1536), dict(out=A + 2048 + 16, qld=1536), dict(out=A + 0x10000),
+    dict(out=A + 0x11000 - 4080), dict(out=A + 0x12000 + 496), dict(out=A + (1 << 24) + 17392), dict(out=A + (1 << 28) + 4096),
+    dict(lse=A), dict(lse=A + 0x30000 + 4092), dict(lse=A + 0x12000 - 60), dict(lse=A + (1 << 24)), dict(lse=A + (1 << 28) + 64),
+    dict(ws=A), dict(ws=A + 0x10000), dict(ws=A + (1 << 24)),
+])
+def test_kv4_attn_refuses_overlapping_outputs(kw):
+    attn(**kw)

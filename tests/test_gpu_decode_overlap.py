@@ -6,7 +6,7 @@ import torch
 import paper_2606_01751_amd as sx
 import workloads as W
 from sxgpu import desc_of
-from test_gpu_decode import DT, i32
+from test_gpu_decode import DT, Batch, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,17 @@ def test_qk_norm_rope_rows_refuses_shared_tensors():
         with pytest.raises(sx.SxError, match="overlap"):
             sx.qk_norm_rope_rows(plan, a["rows"], n, T, q, a["k"], a["gamma_q"])
     plan.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype,sizes", [
+    (8, 2, 128, "bf16", [(1, 40), (1, 3000), (9, 700), (3, 5000)]), (4, 1, 64, "bf16", [(300, 700), (1, 9000), (200, 4000)]),
+    (6, 2, 64, "f32", [(1, 40), (45, 2500), (7, 300)]),
+])
+def test_kv4_attn_in_place(hq, hkv, d, dtype, sizes):
+    b = Batch(sizes, hq, hkv, d, dtype, seed=hq)
+    want, want_lse = b.run()
+    n, q = b.cu[-1], b.q.clone()
+    size = sx.kv4_attn_workspace(b.desc, len(sizes), max(b.nq), max(b.nk))
+    ws, lse = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty(n + 2, hq, device="cuda")
+    sx.kv4_attn(b.desc, q, i32(b.cu), i32(b.nk), b.table.cuda(), b.pool, q, max(b.nq), max(b.nk), ws, lse=lse)
+    assert torch.equal(q[:n], want[:n]) and torch.equal(q[n:], b.q[n:]) and torch.equal(lse[:n], want_lse[:n])
