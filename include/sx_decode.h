@@ -98,6 +98,8 @@ sx_status sx_qk_norm_rope_rows(const sx_plan* plan, const int32_t* rows, const i
 /* Bytes of one KV head of one block in the 4-bit pool: 17 * head_dim (2176 or 1088). */
 sx_status sx_kv4_record_bytes(const sx_layer_desc* desc, int64_t* bytes);
 
+/* The four moves below: what a call writes must not overlap its other arguments (SX_EINVAL). */
+
 /* Rounds rows k, v [n_tokens][Hkv][d] (rows ld elements apart as above) to 4 bits into slots[i] of the
  * pool; a row whose slot is negative (or beyond the pool) is skipped.  The slots of one call are
  * distinct.  Nothing else in the pool is written. */

@@ -108,6 +108,20 @@ sx_status check_move(const sx_layer_desc* d, const void* pool, int64_t n_blocks,
   return SX_OK;
 }
 
+Rows pool_blocks(const sx_layer_desc* d, const void* pool, int64_t n_blocks) {
+  const int64_t block = (int64_t)d->n_kv_heads * sx::kv4_record(d->head_dim);
+  return {pool, n_blocks, block, block};
+}
+
+// What a move writes (the pool, or k and v) must not overlap anything else of the call.
+sx_status check_apart(Rows k, Rows v, Rows pool, Rows idx, Rows idx2, bool write, const char* who) {
+  if (write ? rows_overlap(pool, k) || rows_overlap(pool, v) || rows_overlap(pool, idx) || rows_overlap(pool, idx2)
+            : rows_overlap(k, v) || rows_overlap(k, pool) || rows_overlap(v, pool) || rows_overlap(k, idx) || rows_overlap(v, idx) ||
+                  rows_overlap(k, idx2) || rows_overlap(v, idx2))
+    return reportf(SX_EINVAL, "%s: an output overlaps another argument", who);
+  return SX_OK;
+}
+
 sx_status move_rows(const sx_layer_desc* d, const void* k, int64_t k_ld, const void* v, int64_t v_ld, const int32_t* slots,
                     int32_t n, const void* pool, int64_t n_blocks, bool write, void* stream, const char* who) {
   sx_status st = check_move(d, pool, n_blocks, slots, n, false, who);
@@ -115,6 +129,10 @@ sx_status move_rows(const sx_layer_desc* d, const void* k, int64_t k_ld, const v
   if ((st = check_rows_arg(d, "k", k, k_ld, d->n_kv_heads)) != SX_OK) return st;
   if ((st = check_rows_arg(d, "v", v, v_ld, d->n_kv_heads)) != SX_OK) return st;
   if ((st = index_ok(slots, n, n_blocks * sx::kBlock, stream, who)) != SX_OK) return st;
+  const int64_t es = esize(d), width = d->n_kv_heads * d->head_dim * es;
+  if ((st = check_apart({k, n, width, k_ld * es}, {v, n, width, v_ld * es}, pool_blocks(d, pool, n_blocks), whole(slots, 4ll * n),
+                        whole(nullptr, 0), write, who)) != SX_OK)
+    return st;
   sx::Kv4MoveK a{};
   a.k = const_cast<void*>(k);
   a.v = const_cast<void*>(v);
@@ -140,6 +158,10 @@ sx_status move_blocks(const sx_layer_desc* d, const void* kc, const void* vc, in
   if (n_cache_blocks < 1 || n_cache_blocks > INT32_MAX) return reportf(SX_ESHAPE, "%s: n_cache_blocks %lld", who, (long long)n_cache_blocks);
   if ((st = index_ok(pb, n, n_blocks, stream, who)) != SX_OK) return st;
   if ((st = index_ok(cb, n, n_cache_blocks, stream, who)) != SX_OK) return st;
+  const int64_t block = (int64_t)d->n_kv_heads * sx::kBlock * d->head_dim * esize(d);
+  if ((st = check_apart({kc, n_cache_blocks, block, block}, {vc, n_cache_blocks, block, block}, pool_blocks(d, pool, n_blocks),
+                        whole(pb, 4ll * n), whole(cb, 4ll * n), write, who)) != SX_OK)
+    return st;
   sx::Kv4MoveK a{};
   a.k = const_cast<void*>(kc);
   a.v = const_cast<void*>(vc);
@@ -391,11 +413,10 @@ sx_status sx_kv4_attn(const sx_layer_desc* desc, const void* q, int64_t q_ld, co
     return reportf(SX_ESHAPE, "sx_kv4_attn needs %lld bytes of workspace, got %lld", (long long)need, (long long)workspace_bytes);
   if (!aligned16(workspace)) return reportf(SX_EINVAL, "workspace is not 16-byte aligned");
   // (a workgroup reads the rows of q that it writes before it writes them, and no other reads them: out may be q)
-  const int64_t es = esize(desc), width = desc->n_q_heads * desc->head_dim * es;
-  const Rows arr[] = {whole(out, total_q * width), whole(lse, 4ll * total_q * desc->n_q_heads), whole(workspace, need),
+  const int64_t es = esize(desc), width = desc->n_q_heads * desc->head_dim * es, floats = 4ll * desc->n_q_heads;
+  const Rows arr[] = {{out, total_q, width, width}, {lse, total_q, floats, floats}, whole(workspace, need),
                       {q, total_q, width, q_ld * es}, whole(cu_q, 4ll * (n_requests + 1ll)), whole(seq_lens, 4ll * n_requests),
-                      whole(block_table, 4ll * n_requests * max_blocks),
-                      whole(pool, n_blocks * desc->n_kv_heads * sx::kv4_record(desc->head_dim))};
+                      whole(block_table, 4ll * n_requests * max_blocks), pool_blocks(desc, pool, n_blocks)};
   const char* const names[] = {"out", "lse", "workspace"};
   for (int o = 0; o < 3; ++o)
     for (int i = o + 1; i < 8; ++i)

@@ -58,3 +58,36 @@ def attn(**kw):
 ])
 def test_kv4_attn_refuses_overlapping_outputs(kw):
     attn(**kw)
+
+
+# 3 rows of 512 bytes, or 4 blocks of 8192; a pool of 4 blocks of 4352
+@pytest.mark.parametrize("kw", [dict(pool=A), dict(pool=A + 0x10000 + 1024), dict(pool=A + 0x20000 - 16), dict(pool=A - 17392)])
+def test_kv4_write_refuses_a_pool_over_its_inputs(kw):
+    a = dict(k=A, v=A + 0x10000, slots=A + 0x20000, pool=A + 0x30000)
+    a.update(kw)
+    err(sx.lib().sx_kv4_write(ctypes.byref(desc()), a["k"], 256, a["v"], 256, a["slots"], 3, a["pool"], 4, None), sx.SX_EINVAL, "overlap")
+
+
+@pytest.mark.parametrize("kw", [
+    dict(v=A), dict(v=A + 1024), dict(k=A + 0x30000 + 17392), dict(v=A + 0x30000 - 1520), dict(k=A + 0x20000), dict(v=A + 0x20000 - 1520),
+    dict(kld=768, vld=768, v=A + 496),
+])
+def test_kv4_read_refuses_outputs_over_arguments(kw):
+    a = dict(k=A, kld=256, v=A + 0x10000, vld=256, slots=A + 0x20000, pool=A + 0x30000)
+    a.update(kw)
+    err(sx.lib().sx_kv4_read(ctypes.byref(desc()), a["pool"], 4, a["slots"], 3, a["k"], a["kld"], a["v"], a["vld"], None), sx.SX_EINVAL,
+        "overlap")
+
+
+@pytest.mark.parametrize("name,kw", [
+    ("pack", dict(pool=A + 32752)), ("pack", dict(pool=A + 0x10000 - 16)), ("pack", dict(pool=A + 0x20000)), ("pack", dict(pb=A + 0x30000)),
+    ("unpack", dict(v=A + 32752)), ("unpack", dict(k=A + 0x30000)), ("unpack", dict(v=A + 0x20000 - 16)), ("unpack", dict(pb=A + 4)),
+])
+def test_kv4_blocks_refuse_outputs_over_arguments(name, kw):
+    a = dict(k=A, v=A + 0x10000, cb=A + 0x20000, pool=A + 0x30000, pb=A + 0x40000)
+    a.update(kw)
+    if name == "pack":
+        st = sx.lib().sx_kv4_pack(ctypes.byref(desc()), a["k"], a["v"], 4, a["cb"], 2, a["pool"], 4, a["pb"], None)
+    else:
+        st = sx.lib().sx_kv4_unpack(ctypes.byref(desc()), a["pool"], 4, a["pb"], 2, a["k"], a["v"], 4, a["cb"], None)
+    err(st, sx.SX_EINVAL, "overlap")

@@ -71,3 +71,22 @@ def test_kv4_attn_in_place(hq, hkv, d, dtype, sizes):
     ws, lse = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty(n + 2, hq, device="cuda")
     sx.kv4_attn(b.desc, q, i32(b.cu), i32(b.nk), b.table.cuda(), b.pool, q, max(b.nq), max(b.nk), ws, lse=lse)
     assert torch.equal(q[:n], want[:n]) and torch.equal(q[n:], b.q[n:]) and torch.equal(lse[:n], want_lse[:n])
+
+
+def test_kv4_moves_between_parts_of_one_allocation():
+    # K and V of stacked rows, read into further parts of them; the pool and the cache as parts of one tensor
+    n, hkv, d = 5, 2, 64
+    x = torch.randn(n, 4 * hkv, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    desc, slots = sx.make_desc(hkv, hkv, d, "bf16", 1e4), i32([3, 17, 1, 30, 8])
+    whole = torch.zeros(2 * hkv * 17 * d + 2 * 2 * hkv * 16 * d * 2, dtype=torch.uint8, device="cuda")
+    pool = whole[:2 * hkv * 17 * d].view(2, hkv, 17 * d)
+    kc, vc = whole[2 * hkv * 17 * d:].view(torch.bfloat16).view(2, 2, hkv, 16, d)
+    sx.kv4_write(desc, x[:, :hkv], x[:, hkv:2 * hkv], slots, pool)
+    sx.kv4_read(desc, pool, slots, x[:, 2 * hkv:3 * hkv], x[:, 3 * hkv:])
+    sx.kv4_unpack(desc, pool, i32([0, 1]), kc, vc, i32([1, 0]))
+    for i, s in enumerate(slots.tolist()):
+        assert torch.equal(x[i, 2 * hkv:3 * hkv], kc[1 - s // 16, :, s % 16]) and torch.equal(x[i, 3 * hkv:], vc[1 - s // 16, :, s % 16])
+    with pytest.raises(sx.SxError, match="overlap"):
+        sx.kv4_read(desc, pool, slots, x[:, 2 * hkv:3 * hkv], x[:, 2 * hkv:3 * hkv])
+    with pytest.raises(sx.SxError, match="overlap"):
+        sx.kv4_unpack(desc, pool, i32([0, 1]), kc, kc, i32([1, 0]))
