@@ -16,6 +16,7 @@ cache over.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import torch
 
@@ -30,6 +31,14 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _int(v, what: str) -> int:
+    """A host number that the C call takes as int32 (ctypes would take it modulo 2^32)."""
+    v = operator.index(v)
+    if -0x80000000 <= v <= 0x7fffffff:
+        return v
+    raise ValueError(f"{what} ({v}) does not fit into 32 bits")
 
 
 def _device(t) -> int:
@@ -97,16 +106,17 @@ def append_slots(ctx_lens, new_lens, free_blocks, block_table, seq_lens, cu_new,
     """Block tables and slot maps of a step in which request r, holding ctx_lens[r] tokens, appends new_lens[r]
     (None: one each).  int32 tensors; writes block_table, seq_lens, cu_new, positions, slots and state = (next
     entry of free_blocks, tokens without a slot)."""
+    block_size = _int(block_size, "block_size")
     n, at = ctx_lens.numel(), _device(ctx_lens)
     _need(new_lens is None or new_lens.numel() == n, "new_lens and ctx_lens differ in length")
     _need(seq_lens.numel() == n and cu_new.numel() == n + 1, "seq_lens needs n and cu_new n + 1 entries")
     _need(block_table.dim() == 2 and block_table.shape[0] == n, "block_table must be [n_requests][max_blocks]")
-    room = positions.numel()
+    room, n_free = _int(positions.numel(), "positions"), _int(free_blocks.numel(), "free_blocks")
     _need(slots.numel() == room, "positions and slots differ in length")
     _need(state.numel() >= 2 and (free_head is None or free_head.numel() >= 1), "state needs two entries, free_head one")
     _check(lib().sx_append_slots(
         _ptr(ctx_lens, _I32, at, "ctx_lens"), _opt(new_lens, _I32, at, "new_lens"), n, block_size,
-        _ptr(free_blocks, _I32, at, "free_blocks"), free_blocks.numel(), _opt(free_head, _I32, at, "free_head"),
+        _ptr(free_blocks, _I32, at, "free_blocks"), n_free, _opt(free_head, _I32, at, "free_head"),
         _ptr(block_table, _I32, at, "block_table"), block_table.shape[1], room, _ptr(seq_lens, _I32, at, "seq_lens"),
         _ptr(cu_new, _I32, at, "cu_new"), _ptr(positions, _I32, at, "positions"), _ptr(slots, _I32, at, "slots"),
         _ptr(state, _I32, at, "state"), _on(stream, at)))
@@ -132,6 +142,7 @@ def qk_norm_rope(desc: LayerDesc, q, k, positions, q_out, k_out, gamma_q=None, g
 def qk_norm_rope_rows(plan: Plan, rows, n_rows, max_rows: int, q, k, gamma_q=None, gamma_k=None, eps: float = 1e-6,
                       stream=None):
     """The same in place on the listed rows of a plan, at their positions in the new sequence (beside rope_rows)."""
+    max_rows = _int(int(max_rows), "max_rows")
     dt, d, at = _TYPES.get(plan.desc.dtype), plan.desc.head_dim, _device(q)
     tokens = plan.info()["total_tokens"]
     for t, heads, what in ((q, plan.desc.n_q_heads, "q"), (k, plan.desc.n_kv_heads, "k")):
@@ -140,7 +151,7 @@ def qk_norm_rope_rows(plan: Plan, rows, n_rows, max_rows: int, q, k, gamma_q=Non
         _need(isinstance(t, int) or t.numel() >= n, f"{what} needs {n} entries")
     _check(lib().sx_qk_norm_rope_rows(plan.handle, rows if isinstance(rows, int) else _ptr(rows, _I32, at, "rows"),
                                       n_rows if isinstance(n_rows, int) else _ptr(n_rows, _I32, at, "n_rows"),
-                                      int(max_rows), _ptr(q, dt, at, "q"), _ptr(k, dt, at, "k"),
+                                      max_rows, _ptr(q, dt, at, "q"), _ptr(k, dt, at, "k"),
                                       _gamma(dt, d, gamma_q, at, "gamma_q"), _gamma(dt, d, gamma_k, at, "gamma_k"), eps,
                                       _on(stream, at)))
 
@@ -196,7 +207,8 @@ def kv4_unpack(desc: LayerDesc, pool, pool_blocks, k_cache, v_cache, cache_block
 def kv4_attn_workspace(desc: LayerDesc, n_requests: int, max_q: int, max_seqlen: int) -> int:
     """Bytes of workspace that kv4_attn needs for these bounds."""
     n = ctypes.c_int64()
-    _check(lib().sx_kv4_attn_workspace(ctypes.byref(desc), n_requests, max_q, max_seqlen, ctypes.byref(n)))
+    _check(lib().sx_kv4_attn_workspace(ctypes.byref(desc), _int(n_requests, "n_requests"), _int(max_q, "max_q"),
+                                       _int(max_seqlen, "max_seqlen"), ctypes.byref(n)))
     return n.value
 
 
@@ -204,6 +216,7 @@ def kv4_attn(desc: LayerDesc, q, cu_q, seq_lens, block_table, pool, out, max_q: 
              lse=None, stream=None):
     """out = causal attention of every request's last tokens (rows cu_q[r] .. cu_q[r + 1] of q) over its seq_lens[r] keys
     in the pool; lse (float32 [total_q][Hq]) their natural-log sums.  workspace: uint8, kv4_attn_workspace bytes."""
+    max_q, max_seqlen = _int(max_q, "max_q"), _int(max_seqlen, "max_seqlen")
     n, total, at, dt = seq_lens.numel(), q.shape[0], _device(seq_lens), _TYPES.get(desc.dtype)
     _need(cu_q.numel() == n + 1, "cu_q needs one entry more than seq_lens")
     _need(block_table.dim() == 2 and block_table.shape[0] == n, "block_table must be [n_requests][max_blocks]")

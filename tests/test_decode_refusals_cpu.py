@@ -3,6 +3,7 @@ do not hold."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2606_01751_amd as sx
 from test_decode_cpu import A, attn_args, desc, err, qk_args
@@ -91,3 +92,20 @@ def test_kv4_blocks_refuse_outputs_over_arguments(name, kw):
     else:
         st = sx.lib().sx_kv4_unpack(ctypes.byref(desc()), a["pool"], 4, a["pb"], 2, a["k"], a["v"], 4, a["cb"], None)
     err(st, sx.SX_EINVAL, "overlap")
+
+
+def test_binding_refuses_sizes_that_the_c_types_do_not_hold():
+    # ctypes takes them modulo 2^32: a bound of 2^32 + 512 keys came out as one of 512
+    for bad in ((8, 1, (1 << 32) + 512), (8, (1 << 32) + 1, 4096), ((1 << 32) + 8, 1, 4096), (8, 1, 1 << 31), (8, -1 << 40, 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            sx.kv4_attn_workspace(desc(), *bad)
+    with pytest.raises(sx.SxError):
+        sx.kv4_attn_workspace(desc(), 8, -1, 4096)
+    with pytest.raises(TypeError):
+        sx.kv4_attn_workspace(desc(), 8, 1.5, 4096)
+    z = torch.zeros(4, 2, 128, dtype=torch.int32)
+    with pytest.raises(ValueError, match="32 bits"):
+        sx.append_slots(*[z] * 9, block_size=(1 << 32) + 16)
+    for bound in (dict(max_q=1, max_seqlen=1 << 32), dict(max_q=1 << 31, max_seqlen=7)):
+        with pytest.raises(ValueError, match="32 bits"):
+            sx.kv4_attn(desc(), z, z, z, z, z, z, workspace=z, **bound)
