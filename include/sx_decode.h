@@ -78,7 +78,8 @@ sx_status sx_append_slots(const int32_t* ctx_lens, const int32_t* new_lens, int3
  * [n_tokens][Hkv][d],
  *   y = x / sqrt(mean x^2 + eps) * gamma        (gamma_q or gamma_k [d]; NULL: y = x, eps not read)
  *   out = y rotated to positions[row]           (pairs and frequencies as in sx_rope_realign)
- * in float32 with one rounding at the end; angle and cos / sin in float64, rounded to float32.
+ * in float32 with one rounding at the end; angle and cos / sin in float64, rounded to float32 (rope_base of at
+ * least 2^-20, SX_EUNSUPPORTED below).
  * positions [n_tokens] int32: a row with a negative position is neither computed nor written.
  * Rows are contiguous, ld elements apart (a multiple of 8, at least heads * d: the parts of a stacked
  * projection).  q_out, k_out may be q, k themselves with the same ld; otherwise their rows must not overlap

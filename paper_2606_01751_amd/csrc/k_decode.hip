@@ -185,7 +185,7 @@ over_requests:
 // ---------------------------------------------------------------------------------------------
 
 // cos and sin of phi >= 0, rounded to float32.  phi = n pi/2 + r with |r| <= pi/4, pi/2 in two float64 parts (the first
-// is off by 2^-54, the second makes up for n times that; positions below 2^31 keep n below 2^31 for bases of 1 and more);
+// is off by 2^-54, the second makes up for n times that; good for phi below 2^52, which the host's bound of the base keeps);
 // the Taylor polynomials of r up to r^13 and r^14 are off by less than 2^-45, far below half a unit of float32.
 __device__ __forceinline__ void cos_sin(double phi, float* c, float* s) {
   const double n = __builtin_rint(phi * 0.63661977236758134308);

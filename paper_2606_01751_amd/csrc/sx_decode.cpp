@@ -190,7 +190,9 @@ const double* frequencies(double base, int d) {
   return table;
 }
 
-sx_status check_norm(const void* gamma_q, const void* gamma_k, float eps) {
+sx_status check_norm(const sx_layer_desc* d, const void* gamma_q, const void* gamma_k, float eps) {
+  // (the kernel's cos and sin hold for angles below 2^52; frequencies are at most 1 / base, positions below 2^31)
+  if (d->rope_base < 0x1p-20) return reportf(SX_EUNSUPPORTED, "rope_base %g below 2^-20", d->rope_base);
   if (!aligned16(gamma_q) || !aligned16(gamma_k)) return reportf(SX_EINVAL, "gamma is not 16-byte aligned");
   if ((gamma_q || gamma_k) && (!(eps > 0.0f) || !std::isfinite(eps))) return reportf(SX_EINVAL, "eps must be finite and > 0");
   return SX_OK;
@@ -268,7 +270,7 @@ sx_status sx_qk_norm_rope(const sx_layer_desc* desc, const void* q, int64_t q_ld
   if ((st = check_rows_arg(desc, "k", k, k_ld, desc->n_kv_heads)) != SX_OK) return st;
   if ((st = check_rows_arg(desc, "q_out", q_out, q_out_ld, desc->n_q_heads)) != SX_OK) return st;
   if ((st = check_rows_arg(desc, "k_out", k_out, k_out_ld, desc->n_kv_heads)) != SX_OK) return st;
-  if ((st = check_norm(gamma_q, gamma_k, eps)) != SX_OK) return st;
+  if ((st = check_norm(desc, gamma_q, gamma_k, eps)) != SX_OK) return st;
   if (!positions) return reportf(SX_EINVAL, "positions is NULL");
   if ((q_out == q && q_out_ld != q_ld) || (k_out == k && k_out_ld != k_ld))
     return reportf(SX_EINVAL, "in place, the rows must be as far apart in the output as in the input");
@@ -312,7 +314,7 @@ sx_status sx_qk_norm_rope_rows(const sx_plan* p, const int32_t* rows, const int3
   if (!aligned16(q) || !aligned16(k)) return reportf(SX_EINVAL, "q or k is not 16-byte aligned");
   if (max_rows < 0) return reportf(SX_EINVAL, "max_rows must be >= 0");
   if (max_rows > p->max_T) return reportf(SX_ESHAPE, "max_rows %d exceeds the longest request (%d)", max_rows, p->max_T);
-  sx_status st = check_norm(gamma_q, gamma_k, eps);
+  sx_status st = check_norm(&p->desc, gamma_q, gamma_k, eps);
   if (st != SX_OK) return st;
   if (max_rows == 0) return SX_OK;
   if ((st = sx::check_row_list(p, rows, n_rows, max_rows, stream, "sx_qk_norm_rope_rows")) != SX_OK) return st;

@@ -28,6 +28,12 @@ def test_qk_norm_rope_refuses_overlapping_rows(kw):
     qk(**kw)
 
 
+def test_qk_norm_rope_refuses_bases_whose_angles_it_cannot_reduce():
+    # angles up to 2^31 / base: from 2^56 on the reduced angle was no longer one, and cos and sin came out beyond 1
+    for base in (1e-9, 2.0 ** -20 * (1 - 2.0 ** -52), 5e-324):
+        err(sx.lib().sx_qk_norm_rope(ctypes.byref(desc(rope_base=base)), *qk_args()), sx.SX_EUNSUPPORTED, "rope_base")
+
+
 def _rows_meet(x, y):
     return any(a < d and c < b for a, b in x for c, d in y)
 
