@@ -15,8 +15,9 @@
  * Status, streams, memory ownership, dtypes and sx_last_error are as in include/sx.h: no call
  * allocates, synchronises the host, aborts or throws, every tensor is caller-owned DEVICE memory on
  * the current device, and desc.dtype is the type of q, k, v, gamma and out.  No call needs a plan but
- * sx_qk_norm_rope_rows, and none keeps anything between calls, so calls may run at the same time on
- * any streams when their outputs and workspaces differ, and any of them can be captured into a graph.
+ * sx_qk_norm_rope_rows, and none keeps anything between calls but the host thread's last table of RoPE
+ * frequencies, which is a function of rope_base and head_dim: calls may run at the same time on any
+ * streams when their outputs and workspaces differ, and any of them can be captured into a graph.
  * Index arrays in device memory are trusted to hold sensible lengths by the release library, but an
  * entry that is out of range is left out and never followed: the checked library (libsx_checked.so)
  * refuses it with SX_EDEVICE, which cannot be done while the stream is captured.
@@ -68,7 +69,7 @@ extern "C" {
  *                in block_table all the same)
  * A later step passes state as its free_head.  Outputs must not overlap the inputs or each other
  * (SX_EINVAL), so a loop in a graph copies seq_lens and state back before its next step.
- * One launch.  n_requests <= 65536, block_size >= 1. */
+ * One launch.  1 <= n_requests <= 65536 (an empty batch is refused), block_size >= 1. */
 sx_status sx_append_slots(const int32_t* ctx_lens, const int32_t* new_lens, int32_t n_requests, int32_t block_size,
                           const int32_t* free_blocks, int32_t n_free, const int32_t* free_head, int32_t* block_table,
                           int32_t max_blocks, int32_t max_tokens, int32_t* seq_lens, int32_t* cu_new,
@@ -125,7 +126,8 @@ sx_status sx_kv4_unpack(const sx_layer_desc* desc, const void* pool, int64_t n_b
                         void* stream);
 
 /* Bytes of workspace that sx_kv4_attn needs for n_requests requests of at most max_q query tokens and
- * max_seqlen keys (partial results of requests whose keys are split). */
+ * max_seqlen keys (partial results of requests whose keys are split): room for every request at both
+ * bounds, at most 65536 * (4 * head_dim + 8) bytes each (of up to 4096 KV heads). */
 sx_status sx_kv4_attn_workspace(const sx_layer_desc* desc, int32_t n_requests, int32_t max_q, int32_t max_seqlen,
                                 int64_t* bytes);
 

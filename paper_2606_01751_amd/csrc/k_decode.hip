@@ -18,7 +18,7 @@ namespace {
 // once more to count its tokens.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSlotRun = 256;    // requests a run, and threads
-constexpr int kSlotTokens = 1;   // tokens per thread (300 requests, 131072 tokens: 6.4 us; 7.2 with 2, 7.9 with 4)
+constexpr int kSlotTokens = 1;   // tokens per thread (300 requests, 131072 tokens: 6.9 us; 6.8 with 2, 7.6 with 4)
 
 struct SlotRun {
   int64_t tok0, blk0;             // prefix sums before the run

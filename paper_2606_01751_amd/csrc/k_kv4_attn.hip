@@ -8,7 +8,8 @@
 // lane; the codes become bfloat16 in registers, two elements an instruction, exactly.  Nothing goes through
 // LDS until the waves of a workgroup, which take the steps of a chunk of keys in turn, add up their parts.
 // Softmax statistics and sums are float32; a probability goes into the product as two bfloat16 parts (float32
-// q: three, and q itself in three), so what is lost there is below the rounding of the output.
+// q: three, and q itself in three), so what is lost there is below the rounding of the output.  The kernel for many
+// rows, further down, has another layout, and one part.
 #include <algorithm>
 #include <type_traits>
 
@@ -500,7 +501,8 @@ __global__ __launch_bounds__(NW * 64, WAVES) void kv4_attn_kernel(Kv4AttnK a, in
   if (tile < few_tiles<T, MT>(q) && c < q.split.n) few_rows_item<T, D, MT, NW>(a, q, r, h, tile, c);
 }
 
-// Workgroups that take items in turn.
+// Workgroups that take items in turn.  (bfloat16, two tiles of d = 128: 9 registers of a lane are spilled for a third wave a
+// SIMD, as in the direct form.)
 template <typename T, int D, int MT, int NW>
 __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 3 : 2) void kv4_attn_items_kernel(Kv4AttnK ka) {
   const int h = blockIdx.x % (uint32_t)ka.Hkv;

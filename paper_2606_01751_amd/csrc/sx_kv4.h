@@ -21,8 +21,9 @@ __host__ __device__ constexpr int kv4_v_scales(int d) { return 16 * d + d / 2; }
 // batch: at least kKv4Chunk keys each, at most kKv4Splits of them, and at most kKv4Parts parts (rows x heads x
 // chunks), which is a workgroup of 256 rows for each of 256 compute units: more rows fill the chip unsplit.  17 to
 // 255 rows count as 256 (128 rows over 65536 keys, 8 heads: 68 us in 32 chunks, 78 in 64); up to 16 as 16.
-// kKv4Chunk: 64 requests of up to 8192 keys 51.7 us at 1024, 55.3 at 512, 53.8 at 2048; 256 requests of 1024 keys
-// 61, 91 and 61 us.
+// kKv4Chunk, at 1024, 512 and 2048: 64 requests of up to 8192 keys (28 / 4 heads, d = 128) 45.5, 50.4 and 47.3 us; 256
+// requests of 1024 keys (32 / 8) 58, 75 and 59; 24 of up to 5 tokens and 6000 keys (16 / 4, d = 64) 19.5, 20.0 and 25.2;
+// 128 of 5 tokens over 4608 keys (32 / 8, d = 128), which alone gain by the longest, 207, 237 and 181.
 constexpr int kKv4Chunk = 1024;
 constexpr int kKv4Splits = 64;
 constexpr int kKv4Parts = 65536;
