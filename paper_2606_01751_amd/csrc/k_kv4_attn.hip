@@ -51,12 +51,14 @@ __device__ __forceinline__ void split_parts(const float (&x)[8], bf16x8_t (&part
   float rest[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) rest[e] = x[e];
+  // the largest bfloat16: a finite value above it must not round to infinity
+  auto first = [](float v) { return FINITE || !__builtin_isfinite(v) ? v : fminf(fmaxf(v, -0x1.fep127f), 0x1.fep127f); };
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      w[e] = pack_bf16x2(rest[2 * e], rest[2 * e + 1]);
+      w[e] = i > 0 ? pack_bf16x2(rest[2 * e], rest[2 * e + 1]) : pack_bf16x2(first(rest[2 * e]), first(rest[2 * e + 1]));
       if (i + 1 < N) asm("" : "+v"(w[e]));   // (the halves are taken from here, not rounded once more)
     }
     part[i] = as_bf16x8(w[0], w[1], w[2], w[3]);

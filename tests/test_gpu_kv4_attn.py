@@ -313,3 +313,24 @@ def test_float32_keeps_its_precision(hq, hkv, d, sizes):
         want = attention64(b, r)[0]
         off = out[b.cu[r]:b.cu[r + 1]].double() - want
         assert (off.square().mean().sqrt() / want.square().mean().sqrt()).item() < 1e-6
+
+
+@pytest.mark.parametrize("nq", [1, 20])
+def test_the_largest_float32_queries(nq):
+    # finite values above the largest bfloat16 (255 * 2^120): their first part is that, not infinity, so that a key element of 0
+    # takes no part in the score and one of 2^-120 a finite one
+    d = 64
+    b = Batch([(nq, 90)], 4, 2, d, "f32", seed=nq)
+    k = torch.randn(90, 2, d, generator=torch.Generator().manual_seed(1))
+    k[:, :, 32:] = 0
+    put(b, 0, range(90), k, torch.randn(90, 2, d))
+    b.q[:, :, 40] = 0
+    want, want_lse = b.run()
+    for big in (torch.finfo(torch.float32).max, -255.5 * 2.0 ** 120, 255.0 * 2.0 ** 120):
+        b.q[:, :, 40] = big
+        out, lse = b.run()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    k[:, :, 40] = 2.0 ** -120 * torch.randint(-6, 7, (90, 2), generator=torch.Generator().manual_seed(2))
+    put(b, 0, range(90), k, torch.randn(90, 2, d))
+    b.q[:, :, 40] = 255.75 * 2.0 ** 120
+    b.check()
