@@ -215,7 +215,8 @@ def kv4_attn_workspace(desc: LayerDesc, n_requests: int, max_q: int, max_seqlen:
 def kv4_attn(desc: LayerDesc, q, cu_q, seq_lens, block_table, pool, out, max_q: int, max_seqlen: int, workspace,
              lse=None, stream=None):
     """out = causal attention of every request's last tokens (rows cu_q[r] .. cu_q[r + 1] of q) over its seq_lens[r] keys
-    in the pool; lse (float32 [total_q][Hq]) their natural-log sums.  workspace: uint8, kv4_attn_workspace bytes."""
+    in the pool; lse (float32 [total_q][Hq]) their natural-log sums.  out may be q itself where its rows are contiguous.
+    workspace: uint8, kv4_attn_workspace bytes."""
     max_q, max_seqlen = _int(max_q, "max_q"), _int(max_seqlen, "max_seqlen")
     n, total, at, dt = seq_lens.numel(), q.shape[0], _device(seq_lens), _TYPES.get(desc.dtype)
     _need(cu_q.numel() == n + 1, "cu_q needs one entry more than seq_lens")
