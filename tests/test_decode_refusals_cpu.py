@@ -13,16 +13,16 @@ def qk(status=sx.SX_EINVAL, text="overlap", dtype="bf16", **kw):
     err(sx.lib().sx_qk_norm_rope(ctypes.byref(desc(dtype=dtype)), *qk_args(**kw)), status, text)
 
 
-# bf16, 8 / 2 heads of 128: a row of q has 2048 bytes, a row of k 512; a qkv row 3072
+# bf16, 8 / 2 heads of 128: a row of q has 2048 bytes, a row of k 512; a row of stacked parts 3584
 @pytest.mark.parametrize("kw", [
     dict(qo=A + 2048), dict(qo=A + 4096 + 2032), dict(qo=A - 4096 - 2032), dict(qo=A + 0x10000), dict(qo=A + 0x10000 + 1520),
     dict(qo=A + 0x20000), dict(qo=A + 0x21000 - 6128), dict(qo=A + 0x22000), dict(ko=A), dict(ko=A + 6128), dict(ko=A + 0x10200),
     dict(ko=A + 0x30000 + 2048), dict(ko=A + 0x21000), dict(ko=A + 0x22000 - 16),
-    # parts of stacked rows, 1536 elements apart: one row behind, the part of q, one head into the other's part
-    dict(qld=1536, kld=1536, k=A + 2048, qo=A + 3072, qold=1536), dict(qld=1536, kld=1536, k=A + 2048, ko=A + 1536, kold=1536),
-    dict(qld=1536, kld=1536, k=A + 2048, qo=A, qold=1536, ko=A + 2048 + 256, kold=1536),
+    # parts of stacked rows, 1792 elements apart: one row behind, the part of q, one head into the other's part
+    dict(qld=1792, kld=1792, k=A + 2048, qo=A + 3584, qold=1792), dict(qld=1792, kld=1792, k=A + 2048, ko=A + 1536, kold=1792),
+    dict(qld=1792, kld=1792, k=A + 2048, qo=A, qold=1792, ko=A + 2048 + 256, kold=1792),
     # rows of different distances
-    dict(qld=1536, qo=A + 3072 + 1024, qold=1544), dict(qld=1536, kld=256, k=A + 2048, ko=A + 2560, kold=2048),
+    dict(qld=1792, qo=A + 3584 + 1024, qold=1800), dict(qld=1792, kld=256, k=A + 2048, ko=A + 2560, kold=2048),
 ])
 def test_qk_norm_rope_refuses_overlapping_rows(kw):
     qk(**kw)
@@ -41,7 +41,7 @@ def _rows_meet(x, y):
 def test_overlap_is_that_of_the_rows():
     # every offset of a short k_out over the rows of q: refused where a row meets a row, else the call goes on to its next
     # check (eps, which comes before, is valid; a negative position pointer is not there to be read: n_tokens rows only)
-    for qld, kold, n in ((1536, 1536, 3), (1536, 256, 3), (1024, 1536, 2), (2048, 1536, 3), (1536, 1544, 4)):
+    for qld, kold, n in ((1792, 1792, 3), (1792, 256, 3), (1024, 1792, 2), (2048, 1792, 3), (1792, 1800, 4)):
         q = [(A + i * qld * 2, A + i * qld * 2 + 2048) for i in range(n)]
         for off in range(-4096, 3 * n * 4096, 1008):
             at = A + off // 16 * 16
@@ -58,7 +58,7 @@ def attn(**kw):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(out=A + 2048), dict(out=A - 2048 - 16), dict(out=A, qld=1536), dict(out=A + 2048 + 16, qld=1536), dict(out=A + 0x10000),
+    dict(out=A + 2048), dict(out=A - 2048 - 16), dict(out=A, qld=1792), dict(out=A + 2048 + 16, qld=1792), dict(out=A + 0x10000),
     dict(out=A + 0x11000 - 4080), dict(out=A + 0x12000 + 496), dict(out=A + (1 << 24) + 17392), dict(out=A + (1 << 28) + 4096),
     dict(lse=A), dict(lse=A + 0x30000 + 4092), dict(lse=A + 0x12000 - 60), dict(lse=A + (1 << 24)), dict(lse=A + (1 << 28) + 64),
     dict(ws=A), dict(ws=A + 0x10000), dict(ws=A + (1 << 24)),
