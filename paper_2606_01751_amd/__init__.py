@@ -31,6 +31,9 @@ __all__ = [
     # decoding over a 4-bit cache (decode.py)
     "append_slots", "qk_norm_rope", "qk_norm_rope_rows", "kv4_record_bytes", "kv4_write", "kv4_read", "kv4_pack",
     "kv4_unpack", "kv4_attn_workspace", "kv4_attn",
+    # layer body in 8-bit floating point (layer8.py)
+    "f8_scale_ld", "f8_pack_weight", "add_rmsnorm_f8", "silu_mul_f8", "gemm_f8", "moe_route_workspace", "moe_route",
+    "gemm_experts_f8", "moe_combine",
 ]
 
 RELEASE_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsx.so")
@@ -51,6 +54,9 @@ EXPORTED = (
     # include/sx_decode.h
     "sx_append_slots", "sx_qk_norm_rope", "sx_qk_norm_rope_rows", "sx_kv4_record_bytes", "sx_kv4_write", "sx_kv4_read",
     "sx_kv4_pack", "sx_kv4_unpack", "sx_kv4_attn_workspace", "sx_kv4_attn",
+    # include/sx_f8.h
+    "sx_f8_scale_ld", "sx_f8_pack_weight", "sx_add_rmsnorm_f8", "sx_silu_mul_f8", "sx_gemm_f8", "sx_moe_route_workspace",
+    "sx_moe_route", "sx_gemm_experts_f8", "sx_moe_combine",
 )
 
 
@@ -136,6 +142,15 @@ def lib() -> ctypes.CDLL:
         L.sx_kv4_unpack.argtypes = [VP, VP, I64, VP, I32, VP, VP, I64, VP, VP]
         L.sx_kv4_attn_workspace.argtypes = [VP, I32, I32, I32, P(I64)]
         L.sx_kv4_attn.argtypes = [VP, VP, I64, VP, VP, VP, I32, I32, I32, I32, I32, VP, I64, VP, VP, VP, I64, VP]
+        L.sx_f8_scale_ld.argtypes = [I32, P(I32)]
+        L.sx_f8_pack_weight.argtypes = [VP, I64, I32, VP, VP, VP]
+        L.sx_add_rmsnorm_f8.argtypes = [VP, VP, VP, I32, VP, I32, VP, VP, F, I32, VP, VP, VP, VP, I32, VP]
+        L.sx_silu_mul_f8.argtypes = [VP, VP, I32, VP, I32, VP, VP, VP]
+        L.sx_gemm_f8.argtypes = [VP, VP, VP, I32, VP, VP, I32, VP, VP, I32, I32, P(I32), VP, P(VP), I32, VP]
+        L.sx_moe_route_workspace.argtypes = [I32, I32, I32, I32, P(I64)]
+        L.sx_moe_route.argtypes = [VP, VP, I32, VP, I32, I32, I32, I32, VP, VP, VP, VP, VP, I64, VP]
+        L.sx_gemm_experts_f8.argtypes = [VP, VP, I32, I32, VP, VP, I32, I32, VP, VP, I32, I32, VP, I32, VP]
+        L.sx_moe_combine.argtypes = [VP, VP, VP, I32, VP, VP, I32, I32, VP, VP, I32, VP]
         for name in EXPORTED:
             if name in ("sx_last_error", "sx_version"):
                 getattr(L, name).restype = ctypes.c_char_p
@@ -359,13 +374,21 @@ def silu_mul_rows(plan: Plan, n_rows, max_rows: int, gate_up, y, stream=None):
                                   _stream(stream)))
 
 
-# ---- decoding over a 4-bit cache (see include/sx_decode.h) ----
+# ---- decoding over a 4-bit cache (see include/sx_decode.h), layer body in 8 bits (see include/sx_f8.h) ----
+
+_DECODE = ("append_slots", "qk_norm_rope", "qk_norm_rope_rows", "kv4_record_bytes", "kv4_write", "kv4_read", "kv4_pack",
+           "kv4_unpack", "kv4_attn_workspace", "kv4_attn")
+_LAYER8 = ("f8_scale_ld", "f8_pack_weight", "add_rmsnorm_f8", "silu_mul_f8", "gemm_f8", "moe_route_workspace", "moe_route",
+           "gemm_experts_f8", "moe_combine")
+
 
 def __getattr__(name):
-    """The calls of decode.py, loaded with torch on their first use."""
-    if name in ("append_slots", "qk_norm_rope", "qk_norm_rope_rows", "kv4_record_bytes", "kv4_write", "kv4_read", "kv4_pack",
-                "kv4_unpack", "kv4_attn_workspace", "kv4_attn"):
-        from . import decode
-        globals()[name] = getattr(decode, name)
-        return globals()[name]
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    """The calls of decode.py and layer8.py, loaded with torch on their first use."""
+    if name in _DECODE:
+        from . import decode as module
+    elif name in _LAYER8:
+        from . import layer8 as module
+    else:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    globals()[name] = getattr(module, name)
+    return globals()[name]

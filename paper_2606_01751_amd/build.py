@@ -51,7 +51,7 @@ def _compile(src: str, debug: bool, checked: bool = False) -> str:
 def build(debug: bool = False, jobs: int = 8) -> str:
     os.makedirs(BUILD, exist_ok=True)
     sources = sorted(glob.glob(os.path.join(CSRC, "*.hip"))) + sorted(glob.glob(os.path.join(CSRC, "*.cpp")))
-    hosts = [os.path.join(CSRC, f) for f in ("sx_host.cpp", "sx_decode.cpp")]   # the sources the device checks change
+    hosts = [os.path.join(CSRC, f) for f in ("sx_host.cpp", "sx_decode.cpp", "sx_f8.cpp")]   # the sources the device checks change
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(lambda s: _compile(s, debug), sources))
         checked = list(ex.map(lambda s: _compile(s, debug, True), hosts))

@@ -11,7 +11,9 @@
 // cu_seqlens: cu[0] = 0 and 0 <= cu[r + 1] - cu[r] <= max_seqlen.
 // The decoding calls (include/sx_decode.h): lengths >= 0, indices (slots, block ids; a free list's from 0) from -1 up to their
 // bound, and for the attention cu_q as cu_seqlens, within total_q, and the block table entries of every key.
+// The 8-bit layer body (include/sx_f8.h): row counts, the experts' offsets, and the order's entries of places in use.
 // The checks read only in-bounds entries: at most T_r rows of a request's own region.
+#include "sx_f8k.h"
 #include "sx_kv4.h"
 
 namespace sx {
@@ -88,6 +90,21 @@ __global__ __launch_bounds__(256) void check_kv4_kernel(Kv4AttnK a) {   // one w
   }
 }
 
+__global__ __launch_bounds__(256) void check_offsets_kernel(const int32_t* __restrict__ off, int n, int n_places) {
+  const int e = blockIdx.x * blockDim.x + threadIdx.x;
+  if (e == 0 && off[0] != 0) report_bad(kCuStart, 0, 0, off[0]);
+  if (e >= n) return;
+  if (off[e + 1] < off[e] || off[e + 1] > n_places) report_bad(kCuLength, e, e + 1, off[e + 1]);
+}
+
+__global__ __launch_bounds__(256) void check_order_kernel(const int32_t* __restrict__ off, int n_experts,
+                                                          const int32_t* __restrict__ order, int n_places, int gather, int x_rows) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= min(max(off[n_experts], 0), n_places)) return;
+  const int o = order[i];
+  if (o < 0 || o >= n_places || (gather ? o / gather : 0) >= x_rows) report_bad(kBadIndex, 0, i, o);
+}
+
 // Launch status, then the verdict (synchronises the stream).  *code = 0 when valid.
 hipError_t read_verdict(hipStream_t s, int out[4]) {
   hipError_t e = hipGetLastError();
@@ -123,6 +140,20 @@ hipError_t device_check_lengths(const int32_t* ctx, const int32_t* add, int32_t 
 hipError_t device_check_index(const int32_t* idx, int32_t n, int32_t low, int64_t limit, hipStream_t s, int verdict[4]) {
   hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
   hipLaunchKernelGGL(check_index_kernel, dim3((unsigned)(((int64_t)n + 255) / 256)), dim3(256), 0, s, idx, n, low, limit);
+  return read_verdict(s, verdict);
+}
+
+hipError_t device_check_offsets(const int32_t* offsets, int32_t n_experts, int32_t n_places, hipStream_t s, int verdict[4]) {
+  hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
+  hipLaunchKernelGGL(check_offsets_kernel, dim3((unsigned)(n_experts + 255) / 256), dim3(256), 0, s, offsets, n_experts, n_places);
+  return read_verdict(s, verdict);
+}
+
+hipError_t device_check_order(const int32_t* offsets, int32_t n_experts, const int32_t* order, int32_t n_places, int32_t gather,
+                              int32_t x_rows, hipStream_t s, int verdict[4]) {
+  hipLaunchKernelGGL(check_clear_kernel, dim3(1), dim3(64), 0, s);
+  hipLaunchKernelGGL(check_order_kernel, dim3((unsigned)(((int64_t)n_places + 255) / 256)), dim3(256), 0, s, offsets, n_experts,
+                     order, n_places, gather, x_rows);
   return read_verdict(s, verdict);
 }
 
