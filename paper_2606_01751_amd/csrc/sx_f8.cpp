@@ -229,7 +229,7 @@ sx_status sx_gemm_f8(const sx_plan* plan, const int32_t* rows, const int32_t* n_
   // (the smallest tile of the launches: 16 rows x 16 features)
   if (((int64_t)max_rows + 15) / 16 * a.r.n_req * (n / 16) > kMaxGrid)
     return reportf(SX_EUNSUPPORTED, "%s: %d rows x %lld features exceed one launch", who, max_rows, (long long)n);
-  return sx::launch_status(sx::launch_gemm_f8(a, (hipStream_t)stream), "sx_gemm_f8 launch");
+  return sx::launch_status(sx::launch_gemm_f8(a, sx::cu_count(), (hipStream_t)stream), "sx_gemm_f8 launch");
 }
 
 sx_status sx_moe_route_workspace(int32_t n_experts, int32_t top_k, int32_t n_requests, int32_t max_rows, int64_t* bytes) {
@@ -328,7 +328,7 @@ sx_status sx_gemm_experts_f8(const int32_t* offsets, const int32_t* order, int32
   a.scatter = scatter != 0;
   if ((rows / 16 + std::min<int64_t>(n_experts, rows)) * (n / 16) > kMaxGrid)
     return reportf(SX_EUNSUPPORTED, "%s: %d places x %d features exceed one launch", who, n_places, n);
-  return sx::launch_status(sx::launch_gemm_f8(a, (hipStream_t)stream), "sx_gemm_experts_f8 launch");
+  return sx::launch_status(sx::launch_gemm_f8(a, sx::cu_count(), (hipStream_t)stream), "sx_gemm_experts_f8 launch");
 }
 
 sx_status sx_moe_combine(const sx_plan* plan, const int32_t* rows, const int32_t* n_rows, int32_t max_rows,

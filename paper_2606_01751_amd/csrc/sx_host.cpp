@@ -876,6 +876,20 @@ int current_cu_count(int dev) {
   return n > 0 ? n : 0;
 }
 
+}  // namespace
+
+extern "C++" {
+namespace sx {
+int cu_count() {
+  int dev = 0;
+  const int n = hipGetDevice(&dev) == hipSuccess ? current_cu_count(dev) : 0;
+  return n > 0 ? n : 256;
+}
+}  // namespace sx
+}
+
+namespace {
+
 // Work-queue slot of a persistent full-attention launch on device dev: the slots are handed out in
 // turn, so launches that overlap in time use different slots as long as fewer than
 // kDenseQueueSlots are in flight on the device.  -1 (one workgroup per item, no counters) while the

@@ -166,6 +166,8 @@ sx_status reportf(sx_status st, const char* fmt, ...) __attribute__((format(prin
 sx_status check_desc(const sx_layer_desc* d);
 sx_status launch_status(hipError_t e, const char* what);
 float softmax_scale(const sx_layer_desc* d);
+// compute units of the current device
+int cu_count();
 sx_status check_row_list(const sx_plan* p, const int32_t* rows, const int32_t* n_rows, int32_t max_rows, void* stream,
                          const char* who);
 
