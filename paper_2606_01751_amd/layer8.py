@@ -38,48 +38,52 @@ from .decode import _device, _int, _need, _on, _opt, _ptr
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 _CODES = (torch.float8_e4m3fn, torch.uint8)
 _SCALES = (torch.uint8, torch.float8_e8m0fnu)
+_INTS = [ctypes.c_int32 * c for c in range(5)]
+_POINTERS = [ctypes.c_void_p * c for c in range(5)]
 
 
 def _ld(k: int) -> int:
-    return (k // 128 + 3) // 4 * 4
+    return (k + 511) // 512 * 4
 
+
+# (A call's host time is mostly these checks: each tensor's common case is one expression, told apart only where it fails.)
 
 def _matrix(t, dtypes, rows: int, width: int, at: int, what: str):
     """Device pointer of a contiguous [rows][width] tensor (leading dimensions flattened) of one of these types."""
-    shape = t.shape
-    if len(shape) < 2 or shape[-1] != width or t.numel() != rows * width:
-        raise ValueError(f"{what} must be [{rows}][{width}], not {list(shape)}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{what} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
+    if t.shape == (rows, width) and t.dtype in dtypes and t.get_device() == at and t.is_contiguous():
+        return t.data_ptr()
+    if t.dim() < 2 or t.shape[-1] != width or t.numel() != rows * width:
+        raise ValueError(f"{what} must be [{rows}][{width}], not {list(t.shape)}")
+    _need(t.dtype in dtypes, f"{what} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
     return _ptr(t, t.dtype, at, what)
 
 
 def _wide(t, rows: int, at: int, what: str):
     """(pointer, width) of contiguous bfloat16 rows, the trailing dimensions flattened."""
-    _need(t.dim() >= 2 and t.shape[0] == rows, f"{what} must have {rows} rows, not {list(t.shape)}")
-    return _ptr(t, _BF16, at, what), t.numel() // rows if rows else t.shape[1:].numel()
+    shape = t.shape
+    if len(shape) == 2 and shape[0] == rows and t.dtype is _BF16 and t.get_device() == at and t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    _need(len(shape) >= 2 and shape[0] == rows, f"{what} must have {rows} rows, not {list(shape)}")
+    return _ptr(t, _BF16, at, what), shape[1:].numel()
 
 
-def _opt_wide(t, rows: int, width: int, at: int, what: str):
+def _like(t, rows: int, width: int, at: int, what: str):
+    """Pointer of bfloat16 rows of this width, or None."""
     if t is None:
         return None
+    if t.shape == (rows, width) and t.dtype is _BF16 and t.get_device() == at and t.is_contiguous():
+        return t.data_ptr()
     p, w = _wide(t, rows, at, what)
     _need(w == width, f"{what} must be [{rows}][{width}], not {list(t.shape)}")
     return p
-
-
-def _f8(codes, scale, rows: int, at: int, what: str):
-    """(codes, scales, k) of 8-bit rows."""
-    _need(codes.dim() >= 2, f"{what} must be [{rows}][k]")
-    k = codes.shape[-1]
-    return (_matrix(codes, _CODES, rows, k, at, what), _matrix(scale, _SCALES, rows, _ld(k), at, what + "'s scales"), k)
 
 
 def _index(t, n: int, at: int, what: str):
     """Pointer of an int32 array of at least n entries; row lists of a plan come as pointers too."""
     if t is None or isinstance(t, int):
         return t
-    _need(t.numel() >= n, f"{what} needs {n} entries")
+    if t.numel() < n:
+        raise ValueError(f"{what} needs {n} entries")
     return _ptr(t, _I32, at, what)
 
 
@@ -87,9 +91,9 @@ def _row_args(plan, rows, n_rows, max_rows, have: int, at: int):
     """(plan handle, rows, n_rows, max_rows) of a call whose arrays have `have` rows."""
     if plan is None:
         _need(rows is None, "a row list needs a plan")
-        n = have if max_rows is None else _int(max_rows, "max_rows")
+        n = _int(have if max_rows is None else max_rows, "max_rows")
         _need(n <= have, f"max_rows {n} exceeds the arrays' {have} rows")
-        return None, None, _index(n_rows, 1, at, "n_rows"), n
+        return None, None, None if n_rows is None else _index(n_rows, 1, at, "n_rows"), n
     info = plan.info()
     total = info["total_tokens"]
     _need(have == total, f"the arrays have {have} rows, the plan {total} tokens")
@@ -121,23 +125,26 @@ def add_rmsnorm_f8(x, y8, y_scale, gamma=None, eps: float = 1e-6, delta=None, x_
     not) and, in bfloat16, into y16."""
     at, have = _device(x), x.shape[0]
     xp, h = _wide(x, have, at, "x")
-    _need((y8 is None) == (y_scale is None), "y8 and y_scale come together")
-    yp, sp, k = (None, None, h) if y8 is None else _f8(y8, y_scale, have, at, "y8")
-    _need(k == h, f"y8 must be [{have}][{h}], not {list(y8.shape) if y8 is not None else None}")
+    if y8 is None or y_scale is None:
+        _need(y8 is y_scale, "y8 and y_scale come together")
+        yp = sp = None
+    else:
+        yp, sp = _matrix(y8, _CODES, have, h, at, "y8"), _matrix(y_scale, _SCALES, have, _ld(h), at, "y_scale")
     _need(gamma is None or gamma.numel() == h, f"gamma must have {h} elements")
     p, rp, np_, m = _row_args(plan, rows, n_rows, max_rows, have, at)
     _check(lib().sx_add_rmsnorm_f8(
-        p, rp, np_, m, xp, int(bool(x_by_token)), _opt_wide(delta, have, h, at, "delta"), _opt(gamma, _BF16, at, "gamma"),
-        eps, h, _opt_wide(x_out, have, h, at, "x_out"), _opt_wide(y16, have, h, at, "y16"), yp, sp, int(bool(y_by_token)),
-        _on(stream, at)))
+        p, rp, np_, m, xp, 1 if x_by_token else 0, _like(delta, have, h, at, "delta"), _opt(gamma, _BF16, at, "gamma"), eps, h,
+        _like(x_out, have, h, at, "x_out"), _like(y16, have, h, at, "y16"), yp, sp, 1 if y_by_token else 0, _on(stream, at)))
 
 
 def silu_mul_f8(gate_up, y8, y_scale, plan: Plan = None, n_rows=None, max_rows=None, stream=None):
     """y = silu(gate) * up of rows [gate | up] of gate_up [..][2f], in 8 bits."""
     at, have = _device(gate_up), gate_up.shape[0]
     gp, w = _wide(gate_up, have, at, "gate_up")
-    yp, sp, f = _f8(y8, y_scale, have, at, "y8")
-    _need(w == 2 * f, f"gate_up must be [{have}][{2 * f}], not {list(gate_up.shape)}")
+    f = y8.shape[-1]
+    yp, sp = _matrix(y8, _CODES, have, f, at, "y8"), _matrix(y_scale, _SCALES, have, _ld(f), at, "y_scale")
+    if w != 2 * f:
+        raise ValueError(f"gate_up must be [{have}][{2 * f}], not {list(gate_up.shape)}")
     p, _, np_, m = _row_args(plan, None, n_rows, max_rows, have, at)
     _check(lib().sx_silu_mul_f8(p, np_, m, gp, f, yp, sp, _on(stream, at)))
 
@@ -149,17 +156,17 @@ def gemm_f8(x8, x_scale, w8, w_scale, y, residual=None, plan: Plan = None, rows=
     ys = list(y) if isinstance(y, (list, tuple)) else [y]
     _need(1 <= len(ys) <= 4, "y must be one to four tensors")
     at, have = _device(x8), x8.shape[0]
-    xp, xsp, k = _f8(x8, x_scale, have, at, "x8")
+    k = x8.shape[-1]
+    xp, xsp = _matrix(x8, _CODES, have, k, at, "x8"), _matrix(x_scale, _SCALES, have, _ld(k), at, "x_scale")
     outs = [_wide(t, have, at, "y") for t in ys]
-    n = sum(w for _, w in outs)
+    n = _int(sum([w for _, w in outs]), "the parts' width")
     wp = _matrix(w8, _CODES, n, k, at, "w8")
-    wsp = _matrix(w_scale, _SCALES, n // 128, _ld(k), at, "w8's scales")
+    wsp = _matrix(w_scale, _SCALES, n // 128, _ld(k), at, "w_scale")
     p, rp, np_, m = _row_args(plan, rows, n_rows, max_rows, have, at)
     c = len(ys)
     _check(lib().sx_gemm_f8(
-        p, rp, np_, m, xp, xsp, int(bool(x_by_token)), wp, wsp, k, c, (ctypes.c_int32 * c)(*[_int(w, "width") for _, w in outs]),
-        _opt_wide(residual, have, n, at, "residual"), (ctypes.c_void_p * c)(*[q for q, _ in outs]), int(bool(y_by_token)),
-        _on(stream, at)))
+        p, rp, np_, m, xp, xsp, 1 if x_by_token else 0, wp, wsp, k, c, _INTS[c](*[w for _, w in outs]),
+        _like(residual, have, n, at, "residual"), _POINTERS[c](*[q for q, _ in outs]), 1 if y_by_token else 0, _on(stream, at)))
 
 
 def moe_route_workspace(n_experts: int, top_k: int, max_rows: int, n_requests: int = 1) -> int:
@@ -191,7 +198,8 @@ def gemm_experts_f8(x8, x_scale, w8, w_scale, offsets, order, y, gather: int = 0
     """y [places][n]: place p of expert e (offsets[e] <= p < offsets[e + 1]) times w8[e] ([experts][n][k]).  The row of x is p,
     or order[p] // gather; the row of y is p, or with scatter order[p].  order may be None without gather and scatter."""
     at, places, x_rows = _device(x8), y.shape[0], x8.shape[0]
-    xp, xsp, k = _f8(x8, x_scale, x_rows, at, "x8")
+    k = x8.shape[-1]
+    xp, xsp = _matrix(x8, _CODES, x_rows, k, at, "x8"), _matrix(x_scale, _SCALES, x_rows, _ld(k), at, "x_scale")
     yp, n = _wide(y, places, at, "y")
     _need(w8.dim() == 3, "w8 must be [experts][n][k]")
     e = w8.shape[0]
@@ -199,7 +207,7 @@ def gemm_experts_f8(x8, x_scale, w8, w_scale, offsets, order, y, gather: int = 0
     _check(lib().sx_gemm_experts_f8(
         _ptr(offsets, _I32, at, "offsets"), _index(order, places, at, "order"), e, _int(places, "places"), xp, xsp,
         _int(x_rows, "rows of x"), _int(gather, "gather"), _matrix(w8, _CODES, e * n, k, at, "w8"),
-        _matrix(w_scale, _SCALES, e * (n // 128), _ld(k), at, "w8's scales"), k, n, yp, int(bool(scatter)), _on(stream, at)))
+        _matrix(w_scale, _SCALES, e * (n // 128), _ld(k), at, "w_scale"), k, n, yp, int(bool(scatter)), _on(stream, at)))
 
 
 def moe_combine(y, weights, out, residual=None, plan: Plan = None, rows=None, n_rows=None, max_rows=None,
@@ -213,4 +221,4 @@ def moe_combine(y, weights, out, residual=None, plan: Plan = None, rows=None, n_
     _need(w == h, f"y must be [{have * top}][{h}], not {list(y.shape)}")
     p, rp, np_, m = _row_args(plan, rows, n_rows, max_rows, have, at)
     _check(lib().sx_moe_combine(p, rp, np_, m, yp, _matrix(weights, (_F32,), have, top, at, "weights"), top, h,
-                                _opt_wide(residual, have, h, at, "residual"), op, int(bool(out_by_token)), _on(stream, at)))
+                                _like(residual, have, h, at, "residual"), op, int(bool(out_by_token)), _on(stream, at)))
