@@ -7,12 +7,58 @@ namespace {
 
 constexpr int kRouteThreads = 1024;
 
-// Bits of a float in the order of its value, 0 for what is no candidate (any more); a NaN counts as -inf, -0 as +0.
-__device__ __forceinline__ uint32_t order_key(float v) {
+// Bits of a float in the order of its value; a NaN counts as -inf, -0 as +0.
+__device__ __forceinline__ uint32_t order_bits(float v) {
   const uint32_t u = __float_as_uint(v != v ? -INFINITY : v + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+
+// A logit's key: its order above the expert's, the lower expert larger, so that a row's keys differ and the largest says
+// whose it is; 0 for what is no candidate (any more).  Of bfloat16 logits 16 + 16 bits; of float32 ones 32 + 30 bits in a
+// positive float64 below 2, whose order is that of its bits and whose maximum is one instruction.
+struct Key16 {
+  typedef uint32_t T;
+  typedef uint16_t Logit;
+  static __device__ __forceinline__ T make(Logit x, int e) {
+    return (order_bits(__uint_as_float((uint32_t)x << 16)) & 0xffff0000u) | (uint32_t)(0xffff - e);
+  }
+  static __device__ __forceinline__ T none() { return 0; }
+  static __device__ __forceinline__ T larger(T a, T b) { return max(a, b); }
+  static __device__ __forceinline__ T row_max(T v) { return row16_max(v); }
+  static __device__ __forceinline__ T across(T v, int m) { return (T)__shfl_xor((int)v, m, 64); }
+  static __device__ __forceinline__ int expert(T v) { return 0xffff - (int)(v & 0xffff); }
+  static __device__ __forceinline__ float value(T v) { return order_value(v & 0x80000000u ? v & 0xffff0000u : v | 0xffffu); }
+};
+struct Key32 {
+  typedef double T;
+  static __device__ __forceinline__ T of(uint32_t hi, uint32_t lo) { return __hiloint2double((int)hi, (int)lo); }
+  typedef float Logit;
+  static __device__ __forceinline__ T make(Logit x, int e) {
+    const uint32_t k = order_bits(x);
+    return of(k >> 2, k << 30 | (uint32_t)(0x3fffffff - e));
+  }
+  static __device__ __forceinline__ T none() { return 0.0; }
+  // (no key is a NaN or a subnormal number: nothing to make canonical, as fmax would first)
+  static __device__ __forceinline__ T larger(T a, T b) {
+    T m;
+    asm("v_max_f64 %0, %1, %2" : "=v"(m) : "v"(a), "v"(b));
+    return m;
+  }
+  template <int CTRL>
+  static __device__ __forceinline__ T step(T v) {
+    return larger(v, of(dpp<CTRL>((uint32_t)__double2hiint(v)), dpp<CTRL>((uint32_t)__double2loint(v))));
+  }
+  static __device__ __forceinline__ T row_max(T v) { return step<0x121>(step<0x122>(step<0x124>(step<0x128>(v)))); }
+  static __device__ __forceinline__ T across(T v, int m) { return __shfl_xor(v, m, 64); }
+  static __device__ __forceinline__ int expert(T v) { return 0x3fffffff - (__double2loint(v) & 0x3fffffff); }
+  static __device__ __forceinline__ float value(T v) {
+    return order_value((uint32_t)__double2hiint(v) << 2 | (uint32_t)__double2loint(v) >> 30);
+  }
+};
 
 __device__ __forceinline__ float row16_sum(float v) {
   v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));
@@ -25,9 +71,8 @@ __device__ __forceinline__ float row16_sum(float v) {
 __device__ __forceinline__ float share(float v, float m) { return v == m ? 1.0f : expf(v - m); }
 
 // ---------------------------------------------------------------------------------------------
-// Top experts.  LPR lanes share a row, lane l of them the NV logits from l NV on: the lowest lane that holds the maximum,
-// and there the lowest logit that is it, is the lowest index.  A round finds a row's largest remaining logit in every one
-// of its lanes; the lane that owns it writes it down and takes it out.  Rows n0 .. n0 + 63 of request r, found ids to
+// Top experts.  LPR lanes share a row, lane l of them the NV logits from l NV on.  A round finds a row's largest remaining
+// key in every one of its lanes and takes it out; lane j keeps the j-th.  Rows n0 .. n0 + 63 of request r, found ids to
 // LDS too.
 //
 // Grouping.  A workgroup counts its rows' experts (LDS atomics on whole numbers, whose sums have no order).  Once all
@@ -42,76 +87,71 @@ struct RouteLds {
   uint16_t ids[64][kMoeMaxTop];
 };
 
-template <int NV, int LPR, bool F32>
+template <int NV, int LPR, typename Key>
 __device__ __forceinline__ void top_of_rows(const MoeRouteK& a, int r, int n0, int count, RouteLds& l) {
-  constexpr int RPW = 64 / LPR, RPP = kRouteThreads / LPR;   // rows of a wave, of a pass of the workgroup
+  constexpr int RPP = kRouteThreads / LPR;   // rows of a pass of the workgroup
   const int lane = threadIdx.x & 63, sub = lane % LPR, in_wave = lane / LPR;
   const int E = a.n_experts;
+  typedef typename Key::T T;
+  auto row_sum = [&](float s) {
+    s = row16_sum(s);
+    if constexpr (LPR == 64) {
+      s += __shfl_xor(s, 16, 64);
+      s += __shfl_xor(s, 32, 64);
+    }
+    return s;
+  };
   for (int p = 0; p < 64 / RPP; ++p) {
     const int i = p * RPP + threadIdx.x / LPR, n = n0 + i;
     if (n - in_wave >= count) break;   // (no row of the wave is left; its lanes run together)
     const bool live = n < count;
     const int64_t slot = f8_slot(a.r, r, live ? n : n - in_wave);
-    uint32_t key[NV];
     const int e0 = sub * NV;
+    T key[NV];
+    const typename Key::Logit* x = (const typename Key::Logit*)a.logits + slot * E + e0;
+    if (E % NV == 0) {   // a lane's logits are all there, in one piece, or none is
+      struct __attribute__((aligned(sizeof(typename Key::Logit) * NV < 16 ? sizeof(typename Key::Logit) * NV : 16))) Piece {
+        typename Key::Logit x[NV];
+      } piece{};
+      if (e0 < E) piece = *(const Piece*)x;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      key[v] = 0;
-      if (e0 + v < E) {
-        const int64_t at = slot * E + e0 + v;
-        key[v] = order_key(F32 ? ((const float*)a.logits)[at] : __uint_as_float((uint32_t)((const uint16_t*)a.logits)[at] << 16));
-      }
+      for (int v = 0; v < NV; ++v) key[v] = e0 < E ? Key::make(piece.x[v], e0 + v) : Key::none();
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) key[v] = e0 + v < E ? Key::make(x[v], e0 + v) : Key::none();
     }
-    auto wide_max = [&](uint32_t v) {
-      v = row16_max(v);
-      if constexpr (LPR == 64) {
-        v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-        v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
-      }
-      return v;
-    };
-    float top = 0, all = 0, mine = 0;
+    T mine = Key::none();
+    float top = 0, all = 0;
     for (int j = 0; j < a.top_k; ++j) {
-      uint32_t m = key[0];
+      T m = key[0];
 #pragma unroll
-      for (int v = 1; v < NV; ++v) m = max(m, key[v]);
-      const uint32_t best = wide_max(m);
-      const uint64_t have = __ballot(m == best) >> (in_wave * LPR) & (LPR == 64 ? ~0ull : (1ull << LPR) - 1);
-      const bool owner = (int)__builtin_ctzll(have) == sub;
-      const float value = key_value(best);
+      for (int v = 1; v < NV; ++v) m = Key::larger(m, key[v]);
+      m = Key::row_max(m);
+      if constexpr (LPR == 64) {
+        m = Key::larger(m, Key::across(m, 16));
+        m = Key::larger(m, Key::across(m, 32));
+      }
       if (j == 0) {
-        top = value;
+        top = Key::value(m);
         if (!a.renormalise) {
-          float s = 0;
 #pragma unroll
-          for (int v = 0; v < NV; ++v) s += key[v] ? share(key_value(key[v]), top) : 0.0f;
-          s = row16_sum(s);
-          if constexpr (LPR == 64) {
-            s += __shfl_xor(s, 16, 64);
-            s += __shfl_xor(s, 32, 64);
-          }
-          all = s;
+          for (int v = 0; v < NV; ++v) all += key[v] != Key::none() ? share(Key::value(key[v]), top) : 0.0f;
+          all = row_sum(all);
         }
       }
-      const float w = share(value, top);
-      if (a.renormalise) all += w;
-      if (sub == j) mine = w;
-      int id = 0;
-      bool found = false;
+      if (sub == j) mine = m;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const bool it = owner && !found && key[v] == best;
-        id = it ? e0 + v : id;
-        key[v] = it ? 0u : key[v];
-        found = found || it;
-      }
-      if (owner && live) {
-        l.ids[i][j] = (uint16_t)id;
-        a.ids[slot * a.top_k + j] = id;
-        atomicAdd(&l.base[id], 1);
-      }
+      for (int v = 0; v < NV; ++v) key[v] = key[v] == m ? Key::none() : key[v];
     }
-    if (live && sub < a.top_k) a.weights[slot * a.top_k + sub] = top == -INFINITY ? 0.0f : mine / all;
+    const float w = sub < a.top_k ? share(Key::value(mine), top) : 0.0f;
+    if (a.renormalise) all = row_sum(w);
+    if (sub < a.top_k && live) {
+      const int id = Key::expert(mine);
+      l.ids[i][sub] = (uint16_t)id;
+      a.ids[slot * a.top_k + sub] = id;
+      a.weights[slot * a.top_k + sub] = top == -INFINITY ? 0.0f : w / all;
+      atomicAdd(&l.base[id], 1);
+    }
   }
 }
 
@@ -174,14 +214,14 @@ __device__ __forceinline__ void for_rows(const MoeRouteK& a, F f) {
   }
 }
 
-template <int NV, int LPR, bool F32, bool ONE>
+template <int NV, int LPR, typename Key, bool ONE>
 __global__ __launch_bounds__(kRouteThreads) void route_top_kernel(MoeRouteK a) {
   __shared__ RouteLds l;
   for (int e = threadIdx.x; e < a.n_experts; e += kRouteThreads) l.base[e] = 0;
   __syncthreads();
   int last_r = 0, last_n = 0, last_count = 0, chunks = 0;
   for_rows(a, [&](int r, int n0, int count) {
-    top_of_rows<NV, LPR, F32>(a, r, n0, count, l);
+    top_of_rows<NV, LPR, Key>(a, r, n0, count, l);
     last_r = r;
     last_n = n0;
     last_count = count;
@@ -214,10 +254,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(MoeRouteK a)
   if ((int)threadIdx.x < per * E) {
     const int e = threadIdx.x % E;
     int before = 0, sum = 0;
-    for (int b = threadIdx.x / E; b < a.blocks; b += per) {
-      const int c = a.counts[(int64_t)b * E + e];
-      before += b < (int)blockIdx.x ? c : 0;
-      sum += c;
+    for (int b0 = threadIdx.x / E; b0 < a.blocks; b0 += 8 * per) {
+      int c[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = b0 + i * per < a.blocks ? a.counts[(int64_t)(b0 + i * per) * E + e] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        before += b0 + i * per < (int)blockIdx.x ? c[i] : 0;
+        sum += c[i];
+      }
     }
     atomicAdd(&mine[e], before);
     atomicAdd(&all[e], sum);
@@ -243,12 +288,12 @@ hipError_t launch_top(const MoeRouteK& a, bool f32, hipStream_t s) {
   const bool one = a.blocks == 1 && a.r.n_req == 1 && a.r.max_rows <= 64;
   const dim3 grid((unsigned)a.blocks), block(kRouteThreads);
   if (one) {
-    if (f32) hipLaunchKernelGGL((route_top_kernel<NV, LPR, true, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((route_top_kernel<NV, LPR, false, true>), grid, block, 0, s, a);
+    if (f32) hipLaunchKernelGGL((route_top_kernel<NV, LPR, Key32, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((route_top_kernel<NV, LPR, Key16, true>), grid, block, 0, s, a);
     return hipGetLastError();
   }
-  if (f32) hipLaunchKernelGGL((route_top_kernel<NV, LPR, true, false>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((route_top_kernel<NV, LPR, false, false>), grid, block, 0, s, a);
+  if (f32) hipLaunchKernelGGL((route_top_kernel<NV, LPR, Key32, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((route_top_kernel<NV, LPR, Key16, false>), grid, block, 0, s, a);
   hipLaunchKernelGGL(route_place_kernel, grid, block, 0, s, a);
   return hipGetLastError();
 }

@@ -85,7 +85,7 @@ struct MoeCombineK {
 // more than kMoeBlocks requests, one takes reqs_per_block whole ones.  Every one reads all the others' counts, so there
 // are about kMoeBlocks at most.
 constexpr int kMoeBlocks = 256;
-constexpr int kMoeRows = 256;   // rows of a workgroup, where kMoeBlocks of them are enough
+constexpr int kMoeRows = 64;   // rows of a workgroup, where kMoeBlocks of them are enough
 inline void moe_blocks(int n_req, int max_rows, MoeRouteK* a) {
   a->reqs_per_block = n_req > kMoeBlocks ? (n_req + kMoeBlocks - 1) / kMoeBlocks : 1;
   int64_t per = n_req > kMoeBlocks ? 1 : kMoeBlocks / n_req;
