@@ -14,6 +14,7 @@
 // Every kernel adds the blocks of k one by one in ascending order into one accumulator, so a row's result does not depend
 // on the kernel or tile that the launch's size chose.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -22,7 +23,11 @@
 namespace sx {
 namespace {
 
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
+// the same place in LDS written in one width and read in the other
+typedef i32x2_t Alias2 __attribute__((may_alias));
+typedef i32x4_t Alias4 __attribute__((may_alias));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ i32x8_t operand(i32x4_t a, i32x4_t b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
@@ -39,22 +44,49 @@ struct RowTile {
   int64_t a;   // experts: the first place of expert r
 };
 
-// Row tile number `idx` of the launch; false where there is none.
+// Inclusive prefix sums over the lanes of a wave.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15, 31
+  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+}
+
+// Row tile number `idx` of the launch; false where there is none.  Experts: the tiles of 128 of them at a time, so that one
+// round trip to memory finds most.
 template <int BM, bool EXPERTS>
 __device__ __forceinline__ bool row_tile(const F8GemmK& a, int idx, int lane, RowTile* t) {
   if constexpr (EXPERTS) {
-    auto first = [&](int e) { return min(max(a.offsets[e], 0), a.n_places); };
-    auto len = [&](int e) { return max(first(e + 1) - first(e), 0); };
-    int r, q;
-    locate_request(idx, a.n_experts, [&](int e) { return (len(e) + BM - 1) / BM; }, &r, &q, lane);
-    if (r < 0) return false;
-    r = __builtin_amdgcn_readfirstlane(r);
-    *t = {r, __builtin_amdgcn_readfirstlane(q) * BM, len(r), first(r)};
+    int base = 0;
+    for (int e0 = 0; e0 < a.n_experts; e0 += 128) {
+      int first[2], len[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = e0 + 64 * h + lane;
+        first[h] = min(max(a.offsets[min(e, a.n_experts)], 0), a.n_places);
+        len[h] = max(min(max(a.offsets[min(e + 1, a.n_experts)], 0), a.n_places) - first[h], 0);   // (0 behind the last expert)
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = (len[h] + BM - 1) / BM, upto = base + wave_prefix(c);
+        const uint64_t m = __ballot(upto > idx);
+        if (m != 0) {
+          const int l = (int)__builtin_ctzll(m);
+          const int before = __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(c, l);
+          *t = {e0 + 64 * h + l, (idx - before) * BM, __builtin_amdgcn_readlane(len[h], l), __builtin_amdgcn_readlane(first[h], l)};
+          return true;
+        }
+        base = __builtin_amdgcn_readlane(upto, 63);
+      }
+    }
+    return false;
   } else {
     const int r = idx / a.m_tiles;
     *t = {r, (idx - r * a.m_tiles) * BM, f8_count(a.r, r), 0};
+    return t->m0 < t->nr;
   }
-  return t->m0 < t->nr;
 }
 
 // Where row m of the tile's list lies in x (always a row of x: what is out of range is not stored) and in y (-1: nowhere).
@@ -106,53 +138,76 @@ __device__ __forceinline__ int part_of(const F8GemmK& a, int n) {
   return p;
 }
 
+// Lanes of one wave exchange data through LDS, whose accesses the wave makes in order; what keeps the compiler from handing a
+// lane's own earlier store to its later load.
+__device__ __forceinline__ void wave_exchange() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // A wave's results, FI x RJ fragments, through its own part of LDS (epilogue_lds bytes), so that rows go out in whole runs
-// of 32 FI bytes: a store of the fragments themselves (4 features a lane) touches 16 rows at 32 bytes each.  Rows m0 .. of
-// the tile's list, features nw .. of one part.  A residual is fetched into the same places first.
-template <int FI, int RJ>
-constexpr int epilogue_lds() { return 16 * RJ * (32 * FI + 16) + 16 * RJ * 8; }   // (16 bytes a row against bank conflicts)
-template <int FI, int RJ, bool EXPERTS>
-__device__ __forceinline__ void put_tile(const F8GemmK& a, const RowTile& t, int m0, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
-  constexpr int LD = 32 * FI + 16, ROWS = 16 * RJ, CH = 2 * FI, RPI = 64 / CH;   // 16-byte chunks of a row, rows an instruction
+// of 32 FI bytes: a store of the fragments themselves (4 features a lane) touches 16 rows at 32 bytes each.  yrow (LDS):
+// where the wave's rows lie in y, -1 for none; features nw .. of one part.  16 rows at a time; a residual is fetched ahead,
+// and into the same places first.
+template <int FI>
+constexpr int epilogue_lds() { return 16 * (32 * FI + 16); }   // (16 bytes a row against bank conflicts)
+// AGPR: the sums are in accumulation registers; the empty asm keeps the compiler from fetching all of them at once.
+template <bool AGPR, bool RES, int FI, int RJ>
+__device__ __forceinline__ void put_rows(const F8GemmK& a, const int64_t* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
+  constexpr int LD = 32 * FI + 16, CH = 2 * FI, RPI = 64 / CH, IT = (16 + RPI - 1) / RPI;   // 16-byte chunks of a row, rows an instruction
   static_assert(64 % CH == 0, "whole rows an instruction");
   const int lr = lane % 16, g = lane / 16;
   const int part = part_of(a, nw);
   const int64_t ld = a.pn[part + 1] - a.pn[part];
   const int col = nw - a.pn[part] + lane % CH * 8;
-  int64_t* const yrow = (int64_t*)(lds + ROWS * LD);
+  i32x4_t res[IT];
+  auto row_of = [&](int j, int it) { return RPI > 16 && lane / CH >= 16 ? -1 : yrow[16 * j + it * RPI + lane / CH]; };
+  auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < ROWS; i += 64)
-    if (i + lane < ROWS) yrow[i + lane] = m0 + i + lane < t.nr ? y_row<EXPERTS>(a, t, m0 + i + lane) : -1;
-  if (a.res) {
-#pragma unroll 4
-    for (int i = 0; i < ROWS; i += RPI) {
-      const int row = i + lane / CH;
-      if ((ROWS % RPI == 0 || row < ROWS) && yrow[row] >= 0) *(uint4*)(lds + row * LD + lane % CH * 16) = *(const uint4*)(a.res + yrow[row] * ld + col);
+    for (int it = 0; it < IT; ++it) {
+      const int64_t y = row_of(j, it);
+      res[it] = y >= 0 ? *(const i32x4_t*)(a.res + y * ld + col) : i32x4_t{};
     }
-  }
+  };
+  char* const mine = lds + lane / CH * LD + lane % CH * 16;
+  if constexpr (RES) fetch(0);
 #pragma unroll
-  for (int j = 0; j < RJ; ++j)
+  for (int j = 0; j < RJ; ++j) {
+    if constexpr (RES) {
+#pragma unroll
+      for (int it = 0; it < IT; ++it)
+        if (RPI <= 16 || lane / CH < 16) *(Alias4*)(mine + it * RPI * LD) = res[it];
+      if (j + 1 < RJ) fetch(j + 1);
+    }
+    wave_exchange();
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
-      uint2* const at = (uint2*)(lds + (16 * j + lr) * LD + 32 * i + 8 * g);
+      Alias2* const at = (Alias2*)(lds + lr * LD + 32 * i + 8 * g);
       f32x4_t v = acc[i][j];
-      if (a.res) {
-        const uint2 rv = *at;
-        v[0] += bf16_lo(rv.x);
-        v[1] += bf16_hi(rv.x);
-        v[2] += bf16_lo(rv.y);
-        v[3] += bf16_hi(rv.y);
+      if constexpr (AGPR) asm volatile("" : "+a"(v)::"memory");
+      if constexpr (RES) {
+        const i32x2_t rv = *at;
+        v[0] += bf16_lo((uint32_t)rv[0]);
+        v[1] += bf16_hi((uint32_t)rv[0]);
+        v[2] += bf16_lo((uint32_t)rv[1]);
+        v[3] += bf16_hi((uint32_t)rv[1]);
       }
-      *at = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      *at = i32x2_t{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3])};
     }
-#pragma unroll 4
-  for (int i = 0; i < ROWS; i += RPI) {
-    const int row = i + lane / CH;
-    if (ROWS % RPI != 0 && row >= ROWS) continue;
-    const int64_t y = yrow[row];
-    const uint4 v = *(const uint4*)(lds + row * LD + lane % CH * 16);
-    if (y >= 0) *(uint4*)(a.y[part] + y * ld + col) = v;
+    wave_exchange();
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int64_t y = row_of(j, it);
+      if (y >= 0) *(i32x4_t*)(a.y[part] + y * ld + col) = *(const Alias4*)(mine + it * RPI * LD);
+    }
+    wave_exchange();
   }
+}
+// (One branch: a load that some path leaves in flight would have the compiler wait for all transfers in the next loop.)
+template <bool AGPR, int FI, int RJ>
+__device__ __forceinline__ void put_tile(const F8GemmK& a, const int64_t* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
+  if (a.res) put_rows<AGPR, true>(a, yrow, nw, acc, lds, lane);
+  else put_rows<AGPR, false>(a, yrow, nw, acc, lds, lane);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -236,97 +291,189 @@ __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Tiles of BN features x BM rows, WN x WM waves.  Blocks of k move through NST stages of LDS, global -> LDS directly; a tile
+// Tiles of BN features x BM rows, WN x WM waves; a workgroup takes a.run of them, one beside the other, of the same rows.
+// Blocks of k move through NST stages of LDS, global -> LDS directly, those of the next tile behind the last one's; a tile
 // row (one block, 128 bytes) holds 8 chunks of 16 bytes, XOR-swizzled per row so that the 16 rows of a read hit distinct
-// banks.  While the matrix instructions of a block run, the operands of the next one are read (those of x into the
-// registers that are free after their last use, those of w into a second set), and a stage is refilled as soon as all
-// waves have read it.  The scale bytes go ahead of the first stage the same way, for all of k.
+// banks.  The scale bytes go ahead of the first stage the same way, for all of k and all tiles of the run.
 // ---------------------------------------------------------------------------------------------
 constexpr int kLdsBytes = 163840;   // LDS of a compute unit
-constexpr unsigned kXcds = 8;   // XCDs of the chip, which deals workgroups round-robin
-constexpr int kRowGroup = 8;    // row tiles per group of the tile order
+constexpr unsigned kXcds = 8;       // XCDs of the chip, which deals workgroups round-robin
+constexpr int kRowGroup = 8;        // row tiles per group of the tile order
 
 // s_waitcnt with vmcnt <= n (n < 64), expcnt and lgkmcnt left unconstrained (gfx9 encoding)
 #define SX_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | ((((n) >> 4) & 3) << 14) | (0x7 << 4) | (0xF << 8))
 
 __device__ __forceinline__ int chunk_swz(int c, int row) { return c ^ ((row >> 1) & 7); }   // (two rows per 256-byte line)
 
-// Bytes of LDS: the stages, then the scale bytes of x as [word][BM] words, and those of the tile's blocks of w, each of them
-// padded to whole transfers of 64 words.
+// Bytes of LDS: the stages, the scale bytes of x as [word][BM] words, those of the run's blocks of w, each of them padded to
+// whole transfers of 64 words, and where the rows lie in y.  The results of a run go through a place of their own behind
+// that, those of a single tile through the stages.
 __host__ __device__ constexpr int tile_x_scales(int bm, int ld) { return (bm * ld + 255) / 256 * 256; }
-__host__ __device__ constexpr int tile_w_scales(int ld) { return (ld + 255) / 256 * 256; }
-template <int BN, int BM, int NST>
-constexpr int tile_lds(int ld) {
-  return NST * (BN + BM) * kF8Group + tile_x_scales(BM, ld) + (BN + kF8Group - 1) / kF8Group * tile_w_scales(ld);
+__host__ __device__ constexpr int tile_w_scales(int bn, int ld) { return (bn + kF8Group - 1) / kF8Group * ((ld + 255) / 256 * 256); }
+__host__ __device__ constexpr int tile_fixed(int bn, int bm, int nst, int ld, int run) {
+  return nst * (bn + bm) * kF8Group + tile_x_scales(bm, ld) + run * tile_w_scales(bn, ld) + 8 * bm;
 }
 
+// A block of k of a run: its tile, the block, its stage, and for its transfers: the stage's address in LDS with the wave's
+// first kilobyte, the tile's weights at this block, how many transfers of w the wave has (fewer where the weight ends
+// inside the tile), and all lanes, or none behind the last block.
+struct Place {
+  int tile, b, stage;
+  uint32_t lds;
+  const uint8_t* w;
+  int dw, lanes;
+};
+
+template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
+struct Feed {
+  static constexpr int NW = WN * WM, FI = BN / WN / 16, RJ = BM / WM / 16;
+  static constexpr int STAGE = (BN + BM) * kF8Group;
+  static constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW, ND = PW + PX;   // transfers of 1 KB (8 rows) a wave and block
+  static_assert(PW * NW * 8 == BN && PX * NW * 8 == BM, "transfers spread evenly over the waves");
+  static_assert(BN / WN <= kF8Group, "a wave's features lie in one block of the weight");
+
+  const F8GemmK& a;
+  const int lane, wu, lr, g, wn, wm;
+  int n0, nb, tiles;           // first feature, blocks of k, tiles of the run
+  int dw_last;                 // the wave's transfers of w in the run's last tile
+  int64_t to_next;             // from the last block of a tile's weights to the next tile's first
+  uint32_t woff[PW];
+  const uint8_t* src[PX];
+  uint32_t lds0, xs_at, ws_at;
+  int64_t* yrow;               // of the wave's rows
+  char* out;                   // the wave's place for results
+
+  __device__ __forceinline__ Feed(const F8GemmK& arg, int tid)
+      : a(arg), lane(tid & 63), wu(__builtin_amdgcn_readfirstlane(tid >> 6)), lr(lane % 16), g(lane / 16), wn(wu % WN), wm(wu / WN) {}
+
+  __device__ __forceinline__ Place begin(const uint8_t* w) const {
+    return {0, 0, 0, lds0 + (uint32_t)wu * 1024, w, tiles > 1 ? PW : dw_last, -1};
+  }
+  // (without branches, over which the compiler would move matrix instructions)
+  __device__ __forceinline__ void advance(Place& p) const {
+    const bool wrap = p.stage + 1 == NST, last = p.b + 1 == nb;
+    p.stage = wrap ? 0 : p.stage + 1;
+    p.lds = wrap ? lds0 + (uint32_t)wu * 1024 : p.lds + STAGE;
+    p.w += last ? to_next : kF8Group;
+    p.b = last ? 0 : p.b + 1;
+    p.tile += last ? 1 : 0;
+    p.dw = p.tile + 1 < tiles ? PW : p.tile < tiles ? dw_last : 0;
+    p.lanes = p.tile < tiles ? -1 : 0;
+  }
+
+  // Transfer d of this wave for the block at p; no lane takes part where there is none (a branch would let the compiler move
+  // matrix instructions over it).
+  __device__ __forceinline__ void dma(const Place& p, int d) const {
+    const int dw = __builtin_amdgcn_readfirstlane(p.dw), lanes = __builtin_amdgcn_readfirstlane(p.lanes);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(p.lds);
+    const uint64_t wp = (uint64_t)p.w;
+    const uint64_t w = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(wp >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)wp);
+    if (d < PW)
+      asm volatile("s_cmp_gt_i32 %2, %3\n\ts_cselect_b32 exec_lo, -1, 0\n\ts_cselect_b32 exec_hi, -1, 0\n\ts_add_u32 m0, %4, %5\n\t"
+                   "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(woff[d]), "s"(w), "s"(dw), "n"(d), "s"(lds),
+                   "n"(NW * d * 1024)
+                   : "m0", "scc", "memory");
+    else
+      asm volatile("s_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\ts_add_u32 m0, %2, %3\n\t"
+                   "global_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1" ::"v"(src[d - PW] + p.b * kF8Group), "s"(lanes), "s"(lds),
+                   "n"(BN * kF8Group + NW * (d - PW) * 1024)
+                   : "m0", "scc", "memory");
+  }
+  __device__ __forceinline__ void dma_word(const uint8_t* from, uint32_t to) const {
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
+  }
+
+  // The workgroup's run, its addresses and its scale bytes on their way; false where there is nothing to do.
+  // Tile order: groups of kRowGroup row tiles, the run slowest within a group; block b runs on XCD b mod 8, and each XCD
+  // takes a contiguous part of the order, so its workgroups read the same slices of w and x through one L2.
+  __device__ __forceinline__ bool start(char* smem, Place* fill) {
+    const int n_nt = (a.N + BN - 1) / BN, n_runs = (n_nt + a.run - 1) / a.run;
+    const unsigned per_xcd = gridDim.x / kXcds;   // the grid is a multiple of kXcds
+    const unsigned L = blockIdx.x % kXcds * per_xcd + blockIdx.x / kXcds;
+    const int n_mt = EXPERTS ? a.m_tiles : a.m_tiles * a.r.n_req;
+    const unsigned grp = L / (unsigned)(kRowGroup * n_runs);
+    if (grp * kRowGroup >= (unsigned)n_mt) return false;
+    const int in_g = (int)(L - grp * (kRowGroup * n_runs));
+    const int gm = min(kRowGroup, n_mt - (int)grp * kRowGroup);
+    const int run = in_g / gm;
+    if (run >= n_runs) return false;
+    RowTile t;
+    if (!row_tile<BM, EXPERTS>(a, (int)grp * kRowGroup + in_g % gm, lane, &t)) return false;
+    n0 = run * a.run * BN;
+    tiles = min(a.run, n_nt - run * a.run);
+    nb = a.K / kF8Group;
+    const int K = a.K;
+    const int64_t e = EXPERTS ? t.r : 0;
+    to_next = (int64_t)BN * K - (int64_t)(nb - 1) * kF8Group;
+    dw_last = min((max(a.N - n0 - (tiles - 1) * BN - 8 * wu, 0) + 8 * NW - 1) / (8 * NW), PW);
+    // transfers: 1 KB holds rows 8 q .. 8 q + 7 of a tile; lane l fills row 8 q + l / 8, physical chunk l % 8 with the
+    // logical chunk that chunk_swz maps there (an involution).  A wave moves transfers wu + NW i of both operands.
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      const int row = 8 * (wu + NW * i) + lane / 8;
+      woff[i] = (uint32_t)(row * K + chunk_swz(lane % 8, row) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < PX; ++i) {
+      const int row = 8 * (wu + NW * i) + lane / 8;
+      src[i] = a.x + x_row<EXPERTS>(a, t, min(t.m0 + row, t.nr - 1)) * K + chunk_swz(lane % 8, row) * 16;
+    }
+    lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    *fill = begin(a.w + (e * a.N + n0) * K);
+    const int words = a.ld / 4;
+    const uint32_t xs0 = lds0 + NST * STAGE, ws0 = xs0 + tile_x_scales(BM, a.ld);
+    xs_at = xs0 + 4 * (wm * (BM / WM) + lr);
+    ws_at = ws0 + (n0 % kF8Group + wn * (BN / WN)) / kF8Group * ((a.ld + 255) / 256 * 256);
+    int64_t* const rows = (int64_t*)(smem + tile_fixed(BN, BM, NST, a.ld, a.run) - 8 * BM);
+    yrow = rows + wm * (BM / WM);
+    out = (a.run > 1 ? smem + tile_fixed(BN, BM, NST, a.ld, a.run) : smem) + wu * epilogue_lds<FI>();
+    if (lane + 64 * wu < BM) rows[lane + 64 * wu] = t.m0 + lane + 64 * wu < t.nr ? y_row<EXPERTS>(a, t, t.m0 + lane + 64 * wu) : -1;
+    if constexpr (BM > 64 * NW) static_assert(BM <= 64 * NW, "a row a thread");
+    SX_WAIT_VM(0);   // the indices above are the compiler's loads
+    for (int q = wu; q < tile_x_scales(BM, a.ld) / 256; q += NW) {
+      const int i = min(q * 64 + lane, BM * words - 1);
+      dma_word(a.xs + x_row<EXPERTS>(a, t, min(t.m0 + i % BM, t.nr - 1)) * a.ld + 4 * (i / BM), xs0 + q * 256);
+    }
+    // (a row of w's scale bytes after the other: those of a tile's blocks, tile after tile)
+    const int per = (a.ld + 255) / 256, blocks = (BN + kF8Group - 1) / kF8Group;
+    for (int q = wu; q < tiles * blocks * per; q += NW) {
+      const int row = q / per;
+      const int64_t at = e * (a.N / kF8Group) + min((n0 + row / blocks * BN) / kF8Group + row % blocks, a.N / kF8Group - 1);
+      dma_word(a.ws + at * a.ld + 4 * min((q - row * per) * 64 + lane, words - 1), ws0 + q * 256);
+    }
+    return true;
+  }
+  __device__ __forceinline__ static i32x4_t lds16(uint32_t at) { return *(const __attribute__((address_space(3))) i32x4_t*)(uintptr_t)at; }
+  __device__ __forceinline__ static int lds1(uint32_t at) { return (int)*(const __attribute__((address_space(3))) uint8_t*)(uintptr_t)at; }
+  __device__ __forceinline__ int w_scale(int tile, int b) const { return lds1(ws_at + min(tile, tiles - 1) * tile_w_scales(BN, a.ld) + b); }
+  __device__ __forceinline__ int x_scale(int b, int j) const { return lds1(xs_at + (b >> 2) * (4 * BM) + (b & 3) + j * 64); }
+};
+
+// Large tiles.  While the matrix instructions of a block run, the operands of the next one are read, and a stage is refilled
+// as soon as all waves have read it.
 template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
-  constexpr int NW = WN * WM;
-  constexpr int FI = BN / WN / 16, RJ = BM / WM / 16;       // fragments of a wave
-  constexpr int STAGE = (BN + BM) * kF8Group;
-  constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW, ND = PW + PX;   // transfers of 1 KB (8 rows) a wave and stage
-  constexpr int NM = FI * RJ;
+  typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
+  constexpr int FI = F::FI, RJ = F::RJ, ND = F::ND, STAGE = F::STAGE;
   // transfers that refill a stage are issued from the entry of the next block on: D0 of them beside a block's second half,
   // the others beside the next one's first
   constexpr int D0 = (ND * 3 + 3) / 4;
-  static_assert(PW * NW * 8 == BN && PX * NW * 8 == BM, "transfers spread evenly over the waves");
   static_assert(FI % 2 == 0, "two halves");
-  static_assert(BN / WN <= kF8Group, "a wave's features lie in one block of the weight");
   static_assert((NST - 1) * ND < 64, "transfers in flight");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wu = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Tile order: groups of kRowGroup row tiles, the feature tile slowest within a group; block b runs on XCD b mod 8, and
-  // each XCD takes a contiguous run of tiles, so its workgroups read the same slices of w and x through one L2.
-  const int n_nt = (a.N + BN - 1) / BN;
-  const unsigned per_xcd = gridDim.x / kXcds;   // the grid is a multiple of kXcds
-  const unsigned L = blockIdx.x % kXcds * per_xcd + blockIdx.x / kXcds;
-  const int n_mt = EXPERTS ? a.m_tiles : a.m_tiles * a.r.n_req;
-  const unsigned grp = L / (unsigned)(kRowGroup * n_nt);
-  if (grp * kRowGroup >= (unsigned)n_mt) return;
-  const int in_g = (int)(L - grp * (kRowGroup * n_nt));
-  const int gm = min(kRowGroup, n_mt - (int)grp * kRowGroup);
-  const int nt = in_g / gm;
-  if (nt >= n_nt) return;
-  RowTile t;
-  if (!row_tile<BM, EXPERTS>(a, (int)grp * kRowGroup + in_g % gm, lane, &t)) return;
-  const int n0 = nt * BN, K = a.K, nb = K / kF8Group;
-  const int64_t e = EXPERTS ? t.r : 0;
-
-  // ---- transfers: 1 KB holds rows 8 q .. 8 q + 7 of a tile; lane l fills row 8 q + l / 8, physical chunk l % 8 with the
-  // logical chunk that chunk_swz maps there.  A wave moves transfers wu + NW i of both operands. ----
-  const uint8_t* const w0 = a.w + (e * a.N + n0) * K;
-  const int wrow = 8 * wu + lane / 8;
-  // (chunk_swz is an involution; of an odd number of waves every other transfer has the other half's chunk)
-  const uint32_t woff[2] = {(uint32_t)(wrow * K + chunk_swz(lane % 8, wrow) * 16),
-                            (uint32_t)(wrow * K + chunk_swz(lane % 8, wrow + 8 * (NW % 2)) * 16)};
-  const uint8_t* src[PX];
+  F f(a, threadIdx.x);
+  Place fill;
+  if (!f.start(smem, &fill)) return;
+  Place late = fill, cur = fill;
 #pragma unroll
-  for (int i = 0; i < PX; ++i) {
-    const int row = 8 * (wu + NW * i) + lane / 8;
-    src[i] = a.x + x_row<EXPERTS>(a, t, min(t.m0 + row, t.nr - 1)) * K + chunk_swz(lane % 8, row) * 16;
+  for (int b = 0; b < NST; ++b) {
+    late = fill;
+#pragma unroll
+    for (int d = 0; d < (b == NST - 1 ? D0 : ND); ++d) f.dma(fill, d);
+    f.advance(fill);
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  // transfer d of this wave for block b, into stage b mod NST; no lane takes part behind the last block (a branch would let the
-  // compiler move matrix instructions over it)
-  auto dma = [&](int b, int d) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(b % NST * STAGE) +
-                                                       (uint32_t)(d < PW ? (wu + NW * d) * 1024 : BN * kF8Group + (wu + NW * (d - PW)) * 1024));
-    const int lanes = __builtin_amdgcn_readfirstlane(b < nb ? -1 : 0);
-    if (d < PW) {
-      // (rows behind the weight's last one are read from the tile's first rows and not stored)
-      const int row = n0 + 8 * (wu + NW * d) < a.N ? 8 * NW * d : -8 * wu;
-      const uint8_t* base = w0 + (int64_t)row * K + b * kF8Group;
-      asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(woff[d % 2]), "s"(base),
-                   "s"(at), "s"(lanes)
-                   : "m0", "memory");
-    } else {
-      asm volatile("s_mov_b32 exec_lo, %2\n\ts_mov_b32 exec_hi, %2\n\ts_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1" ::"v"(
-                       src[d - PW] + b * kF8Group),
-                   "s"(at), "s"(lanes)
-                   : "m0", "memory");
-    }
-  };
+  SX_WAIT_VM(((NST - 2) * ND + D0) & 63);   // the scale bytes and the first stage
+  __syncthreads();
   // Before a block is read: this wave's transfers of it have landed (of the NST - 2 blocks behind it they may be in flight) and its
   // reads of the block before are done (the barrier alone does not wait for them), and so are the other waves'; past it
   // the stage of the block before is free.
@@ -335,48 +482,10 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
     SX_WAIT_VM((NST - 2) * ND & 63);
     __syncthreads();
   };
-
-  const int wn = wu % WN, wm = wu / WN;
-  const int lr = lane % 16, g = lane / 16;
-  const int nw = n0 + wn * (BN / WN);          // the wave's first feature
   uint32_t lane_off[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(lr * kF8Group + (chunk_swz(4 * h + g, lr) << 4));
+  for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(f.lr * kF8Group + (chunk_swz(4 * h + f.g, f.lr) << 4));
   f32x4_t acc[FI][RJ];
-#pragma unroll
-  for (int i = 0; i < FI; ++i)
-#pragma unroll
-    for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
-
-  SX_WAIT_VM(0);   // the row indices above are the compiler's loads
-  // ---- scale bytes, then the first stages ----
-  const int words = a.ld / 4;
-  const uint32_t xs0 = lds0 + NST * STAGE, ws0 = xs0 + tile_x_scales(BM, a.ld);
-  auto dma_word = [&](const uint8_t* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
-  };
-  for (int q = wu; q < tile_x_scales(BM, a.ld) / 256; q += NW) {
-    const int i = min(q * 64 + lane, BM * words - 1);
-    dma_word(a.xs + x_row<EXPERTS>(a, t, min(t.m0 + i % BM, t.nr - 1)) * a.ld + 4 * (i / BM), xs0 + q * 256);
-  }
-  for (int q = wu; q < (BN + kF8Group - 1) / kF8Group * (tile_w_scales(a.ld) / 256); q += NW) {
-    const int per = tile_w_scales(a.ld) / 256, blk = q / per;
-    const int64_t at = e * (a.N / kF8Group) + min(n0 / kF8Group + blk, a.N / kF8Group - 1);
-    dma_word(a.ws + at * a.ld + 4 * min((q - blk * per) * 64 + lane, words - 1), ws0 + q * 256);
-  }
-#pragma unroll
-  for (int b = 0; b < NST; ++b)
-#pragma unroll
-    for (int d = 0; d < (b == NST - 1 ? D0 : ND); ++d) dma(b, d);
-  SX_WAIT_VM(((NST - 2) * ND + D0) & 63);   // the scale bytes and the first stage
-  __syncthreads();
-
-  auto lds16 = [](uint32_t at) { return *(const __attribute__((address_space(3))) i32x4_t*)(uintptr_t)at; };
-  auto lds1 = [](uint32_t at) { return (int)*(const __attribute__((address_space(3))) uint8_t*)(uintptr_t)at; };
-  const uint32_t ws_at = ws0 + (n0 % kF8Group + wn * (BN / WN)) / kF8Group * tile_w_scales(a.ld);
-  const uint32_t xs_at = xs0 + 4 * (wm * (BM / WM) + lr);
-  auto w_scale = [&](int b) { return lds1(ws_at + b); };
-  auto x_scale = [&](int b, int j) { return lds1(xs_at + (b >> 2) * (4 * BM) + (b & 3) + j * 64); };
   // A block in two halves, the wave's lower features and its upper ones, against all its rows.  Beside the first half the
   // upper features' operands are read; beside the second, once the next block is entered, its lower features' and its
   // rows' into the registers that are free after their last use.  The order is pinned: matrix instruction m, then the reads
@@ -384,9 +493,9 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
   constexpr int FH = FI / 2, HM = FH * RJ, P0 = FH;   // P0: matrix instructions of the second half before the next block is entered
   i32x8_t fw[FI], fx[RJ];
   int sx[RJ], sw;
-  const uint32_t wb = lds0 + (uint32_t)(wn * FI * 16 * kF8Group), xb = lds0 + (uint32_t)((BN + wm * RJ * 16) * kF8Group);
-  auto read = [&](const uint32_t (&base)[2], int f) {
-    return operand(lds16(base[0] + (uint32_t)(f * 16 * kF8Group)), lds16(base[1] + (uint32_t)(f * 16 * kF8Group)));
+  const uint32_t wb = f.lds0 + (uint32_t)(f.wn * FI * 16 * kF8Group), xb = f.lds0 + (uint32_t)((BN + f.wm * RJ * 16) * kF8Group);
+  auto read = [&](const uint32_t (&base)[2], int i) {
+    return operand(F::lds16(base[0] + (uint32_t)(i * 16 * kF8Group)), F::lds16(base[1] + (uint32_t)(i * 16 * kF8Group)));
   };
   auto mfma = [&](int i, int j) { acc[i][j] = mfma_block<0>(fw[i], fx[j], acc[i][j], sw, sx[j]); };
   {
@@ -394,214 +503,151 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
 #pragma unroll
     for (int j = 0; j < RJ; ++j) {
       fx[j] = read(x0, j);
-      sx[j] = x_scale(0, j);
+      sx[j] = f.x_scale(0, j);
     }
 #pragma unroll
     for (int i = 0; i < FH; ++i) fw[i] = read(w0, i);
   }
-  sw = w_scale(0);
+  sw = f.w_scale(0, 0);
   __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (0x7 << 4));   // lgkmcnt 0: else the loop waits for its last reads at its start
-  for (int b = 0; b < nb; ++b) {
-    const int next = min(b + 1, nb - 1);   // (what is read behind the last block is never used)
-    const uint32_t cur = (uint32_t)(b % NST * STAGE), nxt = (uint32_t)((b + 1) % NST * STAGE);
-    // one base register per operand and half of a block (the empty asm keeps the sums from being re-associated into one
-    // register per read)
-    uint32_t wc[2], wx[2], xx[2];
+  for (int tile = 0; tile < f.tiles; ++tile) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      wc[h] = wb + cur + lane_off[h];
-      wx[h] = wb + nxt + lane_off[h];
-      xx[h] = xb + nxt + lane_off[h];
-      asm volatile("" : "+v"(wc[h]), "+v"(wx[h]), "+v"(xx[h]));
-    }
+    for (int i = 0; i < FI; ++i)
 #pragma unroll
-    for (int m = 0; m < HM; ++m) {
-      mfma(m % FH, m / FH);
+      for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
+    for (int b = 0; b < f.nb; ++b) {
+      Place next = cur;
+      f.advance(next);   // (what is read behind the last block is never used)
+      // one base register per operand and half of a block (the empty asm keeps the sums from being re-associated into one
+      // register per read)
+      uint32_t wc[2], wx[2], xx[2];
 #pragma unroll
-      for (int f = 0; f < FH; ++f)
-        if (m == f * (HM > 2 ? HM - 2 : 0) / FH) fw[FH + f] = read(wc, FH + f);
+      for (int h = 0; h < 2; ++h) {
+        wc[h] = wb + cur.stage * STAGE + lane_off[h];
+        wx[h] = wb + next.stage * STAGE + lane_off[h];
+        xx[h] = xb + next.stage * STAGE + lane_off[h];
+        asm volatile("" : "+v"(wc[h]), "+v"(wx[h]), "+v"(xx[h]));
+      }
 #pragma unroll
-      for (int d = D0; d < ND; ++d)
-        if (m == min(1 + (d - D0) * 2, HM - 1)) dma(b - 1 + NST, d);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    int swn = 0;
+      for (int m = 0; m < HM; ++m) {
+        mfma(m % FH, m / FH);
 #pragma unroll
-    for (int m = 0; m < HM; ++m) {
-      mfma(FH + m % FH, m / FH);
-      if (m == P0 - 1) {
+        for (int i = 0; i < FH; ++i)
+          if (m == i * (HM > 2 ? HM - 2 : 0) / FH) fw[FH + i] = read(wc, FH + i);
+#pragma unroll
+        for (int d = D0; d < ND; ++d)
+          if (m == min(1 + (d - D0) * 2, HM - 1)) f.dma(late, d);
         __builtin_amdgcn_sched_barrier(0);
-        enter();
-        swn = w_scale(next);
       }
+      int swn = 0;
 #pragma unroll
-      for (int f = 0; f < FH; ++f)
-        if (m == min(P0 + f * (HM - P0) / FH, HM - 1)) fw[f] = read(wx, f);
-#pragma unroll
-      for (int f = 0; f < RJ; ++f) {
-        if (m == min(max((f + 1) * FH - 1, P0), HM - 1)) {
-          fx[f] = read(xx, f);
-          sx[f] = x_scale(next, f);
+      for (int m = 0; m < HM; ++m) {
+        mfma(FH + m % FH, m / FH);
+        if (m == P0 - 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          enter();
+          swn = f.w_scale(next.tile, next.b);
         }
-      }
 #pragma unroll
-      for (int d = 0; d < D0; ++d)
-        if (m == min(P0 + d * (HM - P0) / D0, HM - 1)) dma(b + NST, d);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < FH; ++i)
+          if (m == min(P0 + i * (HM - P0) / FH, HM - 1)) fw[i] = read(wx, i);
+#pragma unroll
+        for (int j = 0; j < RJ; ++j)
+          if (m == min(max((j + 1) * FH - 1, P0), HM - 1)) {
+            fx[j] = read(xx, j);
+            sx[j] = f.x_scale(next.b, j);
+          }
+#pragma unroll
+        for (int d = 0; d < D0; ++d)
+          if (m == min(P0 + d * (HM - P0) / D0, HM - 1)) f.dma(fill, d);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sw = swn;
+      cur = next;
+      late = fill;
+      f.advance(fill);
     }
-    sw = swn;
+    const int nw = f.n0 + tile * BN + f.wn * (BN / WN);
+    if (a.run == 1) __syncthreads();   // (all waves have read the stages)
+    if (nw < a.N) put_tile<true>(a, f.yrow, nw, acc, f.out, f.lane);
   }
-
-  __syncthreads();   // (all waves have read the stages)
-  if (nw < a.N)
-    put_tile<FI, RJ, EXPERTS>(a, t, t.m0 + wm * RJ * 16, nw, acc, smem + wu * epilogue_lds<FI, RJ>(), lane);
 }
 
-// ---------------------------------------------------------------------------------------------
 // Small tiles: a wave's few matrix instructions a block do not cover the way of its operands from LDS, so KB blocks are
-// taken at once, with one barrier.  Layout and transfers as above; NST is the number of blocks that LDS holds.
-// ---------------------------------------------------------------------------------------------
+// taken at once, with one barrier (KB > 1: of a single tile).  NST is the number of blocks that LDS holds.
 template <int BN, int BM, int WN, int WM, int KB, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
-  constexpr int NW = WN * WM;
-  constexpr int FI = BN / WN / 16, RJ = BM / WM / 16;       // fragments of a wave
-  constexpr int STAGE = (BN + BM) * kF8Group;
-  constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW, ND = PW + PX;   // transfers of 1 KB (8 rows) a wave and stage
-  static_assert(PW * NW * 8 == BN && PX * NW * 8 == BM, "transfers spread evenly over the waves");
-  static_assert(BN / WN <= kF8Group, "a wave's features lie in one block of the weight");
+  typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
+  constexpr int FI = F::FI, RJ = F::RJ, ND = F::ND, STAGE = F::STAGE;
   static_assert(NST % KB == 0 && NST > KB && NST * ND < 64, "transfers in flight");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wu = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Tile order: groups of kRowGroup row tiles, the feature tile slowest within a group; block b runs on XCD b mod 8, and
-  // each XCD takes a contiguous run of tiles, so its workgroups read the same slices of w and x through one L2.
-  const int n_nt = (a.N + BN - 1) / BN;
-  const unsigned per_xcd = gridDim.x / kXcds;   // the grid is a multiple of kXcds
-  const unsigned L = blockIdx.x % kXcds * per_xcd + blockIdx.x / kXcds;
-  const int n_mt = EXPERTS ? a.m_tiles : a.m_tiles * a.r.n_req;
-  const unsigned grp = L / (unsigned)(kRowGroup * n_nt);
-  if (grp * kRowGroup >= (unsigned)n_mt) return;
-  const int in_g = (int)(L - grp * (kRowGroup * n_nt));
-  const int gm = min(kRowGroup, n_mt - (int)grp * kRowGroup);
-  const int nt = in_g / gm;
-  if (nt >= n_nt) return;
-  RowTile t;
-  if (!row_tile<BM, EXPERTS>(a, (int)grp * kRowGroup + in_g % gm, lane, &t)) return;
-  const int n0 = nt * BN, K = a.K, nb = K / kF8Group;
-  const int64_t e = EXPERTS ? t.r : 0;
-
-  // ---- transfers: 1 KB holds rows 8 q .. 8 q + 7 of a tile; lane l fills row 8 q + l / 8, physical chunk l % 8 with the
-  // logical chunk that chunk_swz maps there.  A wave moves transfers wu + NW i of both operands. ----
-  const uint8_t* const w0 = a.w + (e * a.N + n0) * K;
-  const int wrow = 8 * wu + lane / 8;
-  // (chunk_swz is an involution; of an odd number of waves every other transfer has the other half's chunk)
-  const uint32_t woff[2] = {(uint32_t)(wrow * K + chunk_swz(lane % 8, wrow) * 16),
-                            (uint32_t)(wrow * K + chunk_swz(lane % 8, wrow + 8 * (NW % 2)) * 16)};
-  const uint8_t* src[PX];
+  F f(a, threadIdx.x);
+  Place fill;
+  if (!f.start(smem, &fill)) return;
+  int stage = 0;   // of the next block that is read
 #pragma unroll
-  for (int i = 0; i < PX; ++i) {
-    const int row = 8 * (wu + NW * i) + lane / 8;
-    src[i] = a.x + x_row<EXPERTS>(a, t, min(t.m0 + row, t.nr - 1)) * K + chunk_swz(lane % 8, row) * 16;
+  for (int b = 0; b < NST; ++b) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) f.dma(fill, d);
+    f.advance(fill);
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  // transfer d of this wave for block b, into stage b mod NST; no lane takes part behind the last block (a branch would let the
-  // compiler move matrix instructions over it)
-  auto dma = [&](int b, int d) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(b % NST * STAGE) +
-                                                       (uint32_t)(d < PW ? (wu + NW * d) * 1024 : BN * kF8Group + (wu + NW * (d - PW)) * 1024));
-    const int lanes = __builtin_amdgcn_readfirstlane(b < nb ? -1 : 0);
-    if (d < PW) {
-      // (rows behind the weight's last one are read from the tile's first rows and not stored)
-      const int row = n0 + 8 * (wu + NW * d) < a.N ? 8 * NW * d : -8 * wu;
-      const uint8_t* base = w0 + (int64_t)row * K + b * kF8Group;
-      asm volatile("s_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(woff[d % 2]), "s"(base),
-                   "s"(at), "s"(lanes)
-                   : "m0", "memory");
-    } else {
-      asm volatile("s_mov_b32 exec_lo, %2\n\ts_mov_b32 exec_hi, %2\n\ts_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1" ::"v"(
-                       src[d - PW] + b * kF8Group),
-                   "s"(at), "s"(lanes)
-                   : "m0", "memory");
-    }
-  };
-  const int wn = wu % WN, wm = wu / WN;
-  const int lr = lane % 16, g = lane / 16;
-  const int nw = n0 + wn * (BN / WN);          // the wave's first feature
   uint32_t lane_off[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(lr * kF8Group + (chunk_swz(4 * h + g, lr) << 4));
+  for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(f.lr * kF8Group + (chunk_swz(4 * h + f.g, f.lr) << 4));
   f32x4_t acc[FI][RJ];
-#pragma unroll
-  for (int i = 0; i < FI; ++i)
-#pragma unroll
-    for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
-
-  SX_WAIT_VM(0);   // the row indices above are the compiler's loads
-  // ---- scale bytes, then the first stages ----
-  const int words = a.ld / 4;
-  const uint32_t xs0 = lds0 + NST * STAGE, ws0 = xs0 + tile_x_scales(BM, a.ld);
-  auto dma_word = [&](const uint8_t* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
-  };
-  for (int q = wu; q < tile_x_scales(BM, a.ld) / 256; q += NW) {
-    const int i = min(q * 64 + lane, BM * words - 1);
-    dma_word(a.xs + x_row<EXPERTS>(a, t, min(t.m0 + i % BM, t.nr - 1)) * a.ld + 4 * (i / BM), xs0 + q * 256);
-  }
-  for (int q = wu; q < (BN + kF8Group - 1) / kF8Group * (tile_w_scales(a.ld) / 256); q += NW) {
-    const int per = tile_w_scales(a.ld) / 256, blk = q / per;
-    const int64_t at = e * (a.N / kF8Group) + min(n0 / kF8Group + blk, a.N / kF8Group - 1);
-    dma_word(a.ws + at * a.ld + 4 * min((q - blk * per) * 64 + lane, words - 1), ws0 + q * 256);
-  }
-#pragma unroll
-  for (int b = 0; b < NST; ++b)
-#pragma unroll
-    for (int d = 0; d < ND; ++d) dma(b, d);
-  auto lds16 = [](uint32_t at) { return *(const __attribute__((address_space(3))) i32x4_t*)(uintptr_t)at; };
-  auto lds1 = [](uint32_t at) { return (int)*(const __attribute__((address_space(3))) uint8_t*)(uintptr_t)at; };
-  const uint32_t ws_at = ws0 + (n0 % kF8Group + wn * (BN / WN)) / kF8Group * tile_w_scales(a.ld);
-  const uint32_t xs_at = xs0 + 4 * (wm * (BM / WM) + lr);
-  auto w_scale = [&](int b) { return lds1(ws_at + b); };
-  auto x_scale = [&](int b, int j) { return lds1(xs_at + (b >> 2) * (4 * BM) + (b & 3) + j * 64); };
   i32x8_t fw[KB][FI], fx[KB][RJ];
   int sw[KB], sx[KB][RJ];
-  auto read = [&](uint32_t base) { return operand(lds16(base + lane_off[0]), lds16(base + lane_off[1])); };
-  const uint32_t wb = lds0 + (uint32_t)(wn * FI * 16 * kF8Group), xb = lds0 + (uint32_t)((BN + wm * RJ * 16) * kF8Group);
-  for (int b = 0; b < nb; b += KB) {
-    // the KB blocks have landed: all transfers but those of the NST - 2 KB (at first NST - KB) blocks behind them, and all
-    // waves have read the KB before, whose stages are refilled
-    if (b == 0) SX_WAIT_VM((NST - KB) * ND & 63);
-    else SX_WAIT_VM((NST - 2 * KB) * ND & 63);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __syncthreads();
+  auto read = [&](uint32_t base) { return operand(F::lds16(base + lane_off[0]), F::lds16(base + lane_off[1])); };
+  const uint32_t wb = f.lds0 + (uint32_t)(f.wn * FI * 16 * kF8Group), xb = f.lds0 + (uint32_t)((BN + f.wm * RJ * 16) * kF8Group);
+  bool first = true;
+  for (int tile = 0; tile < f.tiles; ++tile) {
 #pragma unroll
-    for (int s = 0; s < KB; ++s) {
-      const uint32_t at = (uint32_t)((b + s) % NST * STAGE);
-      const int c = min(b + s, nb - 1);   // (what is read behind the last block is never used)
+    for (int i = 0; i < FI; ++i)
 #pragma unroll
-      for (int i = 0; i < FI; ++i) fw[s][i] = read(wb + at + (uint32_t)(i * 16 * kF8Group));
+      for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
+    for (int b = 0; b < f.nb; b += KB) {
+      // the KB blocks have landed: all transfers but those of the NST - 2 KB (at first NST - KB) blocks behind them, and all
+      // waves have read the KB before, whose stages are refilled
+      if (first) SX_WAIT_VM((NST - KB) * ND & 63);
+      else SX_WAIT_VM((NST - 2 * KB) * ND & 63);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < RJ; ++j) {
-        fx[s][j] = read(xb + at + (uint32_t)(j * 16 * kF8Group));
-        sx[s][j] = x_scale(c, j);
+      for (int s = 0; s < KB; ++s) {
+        const uint32_t at = (uint32_t)(stage * STAGE);
+        const int c = min(b + s, f.nb - 1);   // (what is read behind the last block is never used)
+        sw[s] = f.w_scale(tile, c);
+#pragma unroll
+        for (int j = 0; j < RJ; ++j) sx[s][j] = f.x_scale(c, j);
+#pragma unroll
+        for (int i = 0; i < FI; ++i) {
+          fw[s][i] = read(wb + at + (uint32_t)(i * 16 * kF8Group));
+          if (i == 0)
+#pragma unroll
+            for (int j = 0; j < RJ; ++j) fx[s][j] = read(xb + at + (uint32_t)(j * 16 * kF8Group));
+        }
+        stage = stage + 1 == NST ? 0 : stage + 1;
       }
-      sw[s] = w_scale(c);
-    }
-    if (b > 0)
+      if (!first)
+#pragma unroll
+        for (int s = 0; s < KB; ++s) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) f.dma(fill, d);
+          f.advance(fill);
+        }
+      first = false;
 #pragma unroll
       for (int s = 0; s < KB; ++s)
+        if (b + s < f.nb)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) dma(b - KB + NST + s, d);
+          for (int i = 0; i < FI; ++i)
 #pragma unroll
-    for (int s = 0; s < KB; ++s)
-      if (b + s < nb)
-#pragma unroll
-        for (int i = 0; i < FI; ++i)
-#pragma unroll
-          for (int j = 0; j < RJ; ++j) acc[i][j] = mfma_block<0>(fw[s][i], fx[s][j], acc[i][j], sw[s], sx[s][j]);
+            for (int j = 0; j < RJ; ++j) acc[i][j] = mfma_block<0>(fw[s][i], fx[s][j], acc[i][j], sw[s], sx[s][j]);
+    }
+    const int nw = f.n0 + tile * BN + f.wn * (BN / WN);
+    if (a.run == 1) __syncthreads();   // (all waves have read the stages)
+    if (nw < a.N) put_tile<false>(a, f.yrow, nw, acc, f.out, f.lane);
   }
-
-  __syncthreads();   // (all waves have read the stages)
-  if (nw < a.N)
-    put_tile<FI, RJ, EXPERTS>(a, t, t.m0 + wm * RJ * 16, nw, acc, smem + wu * epilogue_lds<FI, RJ>(), lane);
 }
 
 // Row tiles of BM rows that the launch may have to take.
@@ -622,51 +668,85 @@ hipError_t launch_stream(F8GemmK& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Grid and LDS of a tiled launch; kernel(experts) is the kernel.
+// Grid and LDS of a tiled launch, in runs of up to `most` tiles: as long as the workgroups of whole rounds then take no
+// more tiles each than in shorter ones.  A run fetches its next tile while it computes and stores the last: 6712 x 28672 x
+// 4096 in 256 x 256 tiles 632 us by runs of 4, 697 singly; 8192 tokens x 8 of 128 experts, 2048 -> 768 554 and 592, 768 -> 2048
+// 206 and 261; of 8 no faster than of 4.
+constexpr int kRun = 4;
 template <int BN, int BM, int WN, int WM, int NST, typename K>
-hipError_t launch_tiled(F8GemmK& a, hipStream_t s, K plain, K experts) {
-  const int64_t m_tiles = count_tiles(a, BM);
+hipError_t launch_tiled(F8GemmK& a, int n_cu, int most, hipStream_t s, K plain, K experts) {
+  const int64_t m_tiles = count_tiles(a, BM), n_tiles = (a.N + BN - 1) / BN;
   a.m_tiles = a.offsets ? (int)m_tiles : (a.r.max_rows + BM - 1) / BM;
-  const int64_t blocks = (m_tiles * ((a.N + BN - 1) / BN) + kXcds - 1) / kXcds * kXcds;
-  const int lds = std::max(tile_lds<BN, BM, NST>(a.ld), WN * WM * epilogue_lds<BN / WN / 16, BM / WM / 16>());
-  if (blocks >= ((int64_t)1 << 31) || lds > kLdsBytes) return hipErrorInvalidConfiguration;
+  constexpr int kOut = WN * WM * epilogue_lds<BN / WN / 16>();
+  int lds = 0;
+  int64_t least = INT64_MAX;
+  for (int run = 1; run <= most; run *= 2) {
+    const int need = tile_fixed(BN, BM, NST, a.ld, run) + (run > 1 ? kOut : 0);
+    if (need > kLdsBytes) break;
+    const int64_t slots = (int64_t)n_cu * (kLdsBytes / need), runs = m_tiles * ((n_tiles + run - 1) / run);
+    const int64_t time = (runs + slots - 1) / slots * run;
+    if (time <= least) {
+      least = time;
+      a.run = run;
+      lds = need;
+    }
+  }
+  const int64_t blocks = (m_tiles * ((n_tiles + a.run - 1) / a.run) + kXcds - 1) / kXcds * kXcds;
+  if (lds == 0 || blocks >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(a.offsets ? experts : plain, dim3((unsigned)blocks), dim3(WN * WM * 64), lds, s, a);
   return hipGetLastError();
 }
 template <int BN, int BM, int WN, int WM, int NST>
-hipError_t launch_tile(F8GemmK& a, hipStream_t s) {
-  return launch_tiled<BN, BM, WN, WM, NST>(a, s, f8_tile_kernel<BN, BM, WN, WM, NST, false>, f8_tile_kernel<BN, BM, WN, WM, NST, true>);
+hipError_t launch_tile(F8GemmK& a, int n_cu, hipStream_t s) {
+  return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, kRun, s, f8_tile_kernel<BN, BM, WN, WM, NST, false>,
+                                           f8_tile_kernel<BN, BM, WN, WM, NST, true>);
 }
 template <int BN, int BM, int WN, int WM, int KB, int NST>
-hipError_t launch_narrow(F8GemmK& a, hipStream_t s) {
-  return launch_tiled<BN, BM, WN, WM, NST>(a, s, f8_narrow_kernel<BN, BM, WN, WM, KB, NST, false>,
+hipError_t launch_narrow(F8GemmK& a, int n_cu, hipStream_t s) {
+  return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, KB == 1 ? kRun : 1, s, f8_narrow_kernel<BN, BM, WN, WM, KB, NST, false>,
                                            f8_narrow_kernel<BN, BM, WN, WM, KB, NST, true>);
 }
 
-// A launch's shape: what a round of workgroups over the compute units (occ on each) takes, per block of k and besides.
+// What a launch of a shape takes, fitted to 90 products of 1 to 6712 rows by six weights of 768 to 14336 x 1024 to 28672 and
+// 26 grouped ones: `first` us and `block` us a block of k for a first round of workgroups, occ on each compute unit,
+// `more` and `more_block` for each further one.
 struct Shape {
   int bn, bm, nst, occ;
-  double block, round;   // us
+  double first, block, more, more_block;
 };
 enum { kStream, k16x16, k64x32, k64x64, k128x64, k128x128, k128x128x2, k256x256, kShapes };
-constexpr Shape kShape[kShapes] = {{16, 16, 0, 1, 0.16, 0.5},    {16, 16, 12, 3, 0.19, 1.2},  {64, 32, 10, 1, 0.245, 1.5},
-                                   {64, 64, 6, 1, 0.27, 1.5},    {128, 64, 3, 2, 0.47, 2},    {128, 128, 4, 1, 0.55, 1.5},
-                                   {128, 128, 2, 2, 1.05, 3},    {256, 256, 2, 1, 1.14, 9}};
+constexpr Shape kShape[kShapes] = {{16, 16, 0, 1, 2.42, 0.124, 0.01, 0.114}, {16, 16, 12, 3, 4.04, 0.206, 2.95, 0.204},
+                                   {64, 32, 10, 1, 4.01, 0.234, 2.76, 0.230}, {64, 64, 6, 1, 3.75, 0.281, 2.65, 0.281},
+                                   {128, 64, 3, 1, 3.40, 0.396, 1.30, 0.316}, {128, 128, 4, 1, 4.06, 0.561, 1.44, 0.605},
+                                   {128, 128, 2, 2, 1.98, 0.808, 5.66, 1.067}, {256, 256, 2, 1, 8.42, 1.240, 4.26, 1.571}};
+constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for grouped rows (of listed ones: 16)
 
-// The shape of least time for listed rows.  Measured (us, K = 4096, weights from memory; the shape taken first, then its
-// neighbours): 16 rows x 4096 features 8.7, 9.5, 11.4; 32 x 6144 10.1, 11.7, 12.3; 64 x 6144 11.8, 12.4, 19.9; 128 x 6144
-// 12.6, 13.8, 21.3; 394 x 4096 16.0, 20.0, 22.7; 1000 x 6144 35.9, 32.5, 38.4; 6712 x 28672 662, 862, 929.
+// The shape of least time: within 8% of the fastest for each of those 90 products (0.4% in the mean), within 13% for the
+// grouped ones (2.4%).  Some of them in us, the shape taken and its neighbours in the table: K = 4096, 1 row x 4096 features
+// 7.0 (10.3), 16 x 6144 10.4 (10.9, 11.4), 96 x 4096 11.7 (22.8, 12.8), 200 x 4096 13.2 (21.5, 15.9), 394 x 4096 16.2 (24.0,
+// 21.7), 1000 x 4096 22.8 (25.0, 28.4), 2048 x 4096 35.4 (41.2, 48.5), 6712 x 28672 631 (845); grouped, 2048 -> 3072, 64 tokens x
+// 8 of 128 experts 126 (130), 512 x 8 of 128 194 (217), 2048 x 2 of 8 42 (49, 59), 8192 x 8 of 128 560 (671).
 int best_shape(const F8GemmK& a, int n_cu) {
-  int best = k64x32;
+  int best = kStream;
   double least = 1e300;
   const double nb = a.K / kF8Group;
   for (int i = 0; i < kShapes; ++i) {
     const Shape& h = kShape[i];
-    const int64_t tiles = count_tiles(a, h.bm) * ((a.N + h.bn - 1) / h.bn);
-    if (h.nst * (h.bn + h.bm) * kF8Group + tile_x_scales(h.bm, a.ld) + (h.bn + kF8Group - 1) / kF8Group * tile_w_scales(a.ld) > kLdsBytes ||
-        tiles >= ((int64_t)1 << 31) - 64)
-      continue;
-    const double t = (double)((tiles + n_cu * h.occ - 1) / (n_cu * h.occ)) * (nb * h.block + h.round);
+    const bool ex = a.offsets, stream = i == kStream;
+    const int bn = ex && stream ? kStreamExperts : h.bn, bm = ex && stream ? kStreamExperts : h.bm;
+    if (ex && (i == k16x16 || i == k64x32 || i == k64x64)) continue;   // (no grouped product measured faster by one)
+    const int64_t n_tiles = (a.N + bn - 1) / bn, most = count_tiles(a, bm) * n_tiles;
+    if ((!stream && (a.ld > kLdsBytes / bm || tile_fixed(bn, bm, h.nst, a.ld, 1) > kLdsBytes)) || most >= ((int64_t)1 << 31) - 64) continue;
+    double tiles = (double)most;
+    if (ex) {   // as many as rows spread over the experts make, each expert's last one half full
+      const double groups = a.n_places < a.n_experts ? a.n_places : a.n_experts, full = a.n_places / groups / bm;
+      tiles = groups * (full > 0.5 ? full + 0.5 : 1) * (double)n_tiles + n_cu / 8;
+      // Few rows an expert: the weights' way from memory is the bound, which the streaming kernel comes nearest to (64 tokens
+      // x 8 of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, 2048 -> 3072: 184, 166).
+      if (stream && a.n_places <= 12 * (int64_t)a.n_experts) return kStream;
+    }
+    const double rounds = ceil(tiles / ((double)n_cu * h.occ));
+    const double t = h.first + nb * h.block + (rounds - 1) * (h.more + nb * h.more_block);
     if (t < least) {
       least = t;
       best = i;
@@ -675,29 +755,18 @@ int best_shape(const F8GemmK& a, int n_cu) {
   return best;
 }
 
-// Grouped rows, by the rows an expert has on average: few, a wave of its own reads each expert's weights past LDS (64 tokens
-// x 8 of 128 experts, 2048 -> 1536: 62 us; 128 x 64 tiles 73, 256 x 256 131); many, 128 x 64 tiles (512 tokens 100; 132, 142)
-// or, from 192 on, the largest of which a block's prologue does not take longer than its products (8192 tokens, 2048 ->
-// 1536: 256 x 256 332, 128 x 128 380; 768 -> 2048: 259 of 128 x 128, 261).
-int expert_shape(const F8GemmK& a) {
-  const double rows = (double)a.n_places / a.n_experts;
-  if (rows <= 12) return kStream;
-  const bool fits = a.ld <= 112;   // (of 256 x 256 tiles)
-  return rows < 192 ? k128x64 : a.K <= 1024 || !fits ? k128x128x2 : k256x256;
-}
-
 }  // namespace
 
 hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
-  switch (a.offsets ? expert_shape(a) : best_shape(a, n_cu)) {
-    case kStream: return a.offsets ? launch_stream<2, 2, 4>(a, s) : launch_stream<1, 1, 8>(a, s);
-    case k16x16: return launch_narrow<16, 16, 1, 1, 4, 12>(a, s);
-    case k64x32: return launch_narrow<64, 32, 4, 1, 2, 10>(a, s);
-    case k64x64: return launch_narrow<64, 64, 2, 2, 2, 6>(a, s);
-    case k128x64: return launch_narrow<128, 64, 4, 2, 1, 3>(a, s);
-    case k128x128: return launch_narrow<128, 128, 4, 2, 1, 4>(a, s);
-    case k128x128x2: return launch_narrow<128, 128, 4, 2, 1, 2>(a, s);
-    default: return launch_tile<256, 256, 2, 2, 2>(a, s);
+  switch (best_shape(a, n_cu)) {
+    case kStream: return a.offsets ? launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4>(a, s) : launch_stream<1, 1, 8>(a, s);
+    case k16x16: return launch_narrow<16, 16, 1, 1, 4, 12>(a, n_cu, s);
+    case k64x32: return launch_narrow<64, 32, 4, 1, 2, 10>(a, n_cu, s);
+    case k64x64: return launch_narrow<64, 64, 2, 2, 2, 6>(a, n_cu, s);
+    case k128x64: return launch_narrow<128, 64, 4, 2, 1, 3>(a, n_cu, s);
+    case k128x128: return launch_narrow<128, 128, 4, 2, 1, 4>(a, n_cu, s);
+    case k128x128x2: return launch_narrow<128, 128, 4, 2, 1, 2>(a, n_cu, s);
+    default: return launch_tile<256, 256, 2, 2, 2>(a, n_cu, s);
   }
 }
 

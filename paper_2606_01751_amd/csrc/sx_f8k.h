@@ -57,6 +57,7 @@ struct F8GemmK {
   int n_parts, K, N, ld, x_tok, y_tok;
   int n_experts, n_places, x_rows, gather, scatter;
   int m_tiles;                // rows: tiles of every request; experts: tiles of the whole launch
+  int run;                    // tiles of features that a workgroup takes one after the other
 };
 
 struct MoeRouteK {

@@ -287,6 +287,59 @@ def test_gemm_f8_is_exact_where_float32_is(rows):
     assert torch.equal(y, (x @ w.t()).float().to(BF16))
 
 
+def codes(g, rows, k, n=None):
+    """Random codes and scale bytes on the GPU, of rows or (with n) of a weight."""
+    c = (torch.randn(n or rows, k, generator=g) * 20).clamp(-448, 448).to(F8).view(torch.uint8).cuda()
+    s = torch.randint(112, 124, ((n or rows) // (128 if n else 1), R.ld(k)), generator=g).to(torch.uint8).cuda()
+    return c, s
+
+
+# launches of every kernel and tile that a call's size can choose, with runs of tiles and weights that end inside one
+LARGE = [(16, 6144, 4096), (40, 4096, 4096), (64, 4224, 4096), (180, 4224, 4096), (394, 4224, 4096), (1000, 3968, 4096),
+         (2048, 4096, 4096), (2500, 11136, 2048), (8100, 8064, 512), (4100, 4992, 128), (6400, 4992, 128), (1450, 8320, 128),
+         (4900, 6528, 896), (700, 12160, 1152), (20, 4224, 16512), (40, 4224, 16512), (200, 2048, 33280), (600, 2048, 16512),
+         (1100, 2048, 16512)]
+
+
+@pytest.mark.parametrize("rows,n,k", LARGE)
+def test_gemm_f8_large_launches(rows, n, k):
+    g = gen(rows + n + k)
+    x, xs = codes(g, rows, k)
+    w, ws = codes(g, 0, k, n)
+    res = torch.randn(rows, n, generator=g).to(BF16).cuda()
+    parts = [n - 768, 128, 640]                        # the middle one inside a tile of 256
+    ys = [torch.full((rows, p), 7.0, dtype=BF16, device="cuda") for p in parts]
+    sx.gemm_f8(x, xs, w, ws, ys)
+    y, z = torch.cat(ys, 1), torch.empty_like(res)
+    sx.gemm_f8(x, xs, w, ws, z, residual=res)
+    # the bits that each row has in a call of its own
+    some = sorted({0, rows - 1, rows // 2, *torch.randint(rows, (6,), generator=g).tolist()})
+    one, two = torch.empty(len(some), n, dtype=BF16, device="cuda"), torch.empty(len(some), n, dtype=BF16, device="cuda")
+    sx.gemm_f8(x[some], xs[some], w, ws, one)
+    sx.gemm_f8(x[some], xs[some], w, ws, two, residual=res[some])
+    assert torch.equal(y[some], one) and torch.equal(z[some], two)
+    # and all rows against calls of 100 rows
+    for lo in range(0, rows, 100):
+        part = torch.empty(min(100, rows - lo), n, dtype=BF16, device="cuda")
+        sx.gemm_f8(x[lo:lo + 100], xs[lo:lo + 100], w, ws, part)
+        assert torch.equal(part, y[lo:lo + 100]), f"rows from {lo}"
+        sx.gemm_f8(x[lo:lo + 100], xs[lo:lo + 100], w, ws, part, residual=res[lo:lo + 100])
+        assert torch.equal(part, z[lo:lo + 100]), f"rows from {lo}, residual"
+    want, mag = R.product(x[some[:3]].cpu(), xs[some[:3]].cpu(), w.cpu(), ws.cpu())
+    near16(one[:3].cpu(), want, R.product_bound(k, mag), "three rows")
+    r = res[some[:3]].cpu().double()
+    near16(two[:3].cpu(), want + r, R.product_bound(k, mag + r.abs()), "three rows, residual")
+
+
+@pytest.mark.parametrize("rows,k", [(5, 65536), (300, 65536), (700, 40064)])
+def test_gemm_f8_of_long_rows(rows, k):
+    g = gen(rows + k)
+    xc, xs, wc, ws = operands(g, rows, 128, k)
+    y, = run_gemm(xc, xs, wc, ws, [128])
+    want, mag = R.product(xc, xs, wc, ws)
+    near16(y, want, R.product_bound(k, mag), f"{rows} x {k}")
+
+
 def test_gemm_f8_parts_and_padded_batches():
     g = gen(4)
     for rows, live in ((37, 30), (70, 64), (200, 1), (5, 0), (20, 25), (300, 290)):

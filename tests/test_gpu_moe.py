@@ -10,7 +10,7 @@ import torch
 
 import f8ref as R
 import paper_2606_01751_amd as sx
-from test_gpu_f8 import BF16, F8, gen, hidden, i32, make_plan, near16, operands, bits8
+from test_gpu_f8 import BF16, F8, codes, gen, hidden, i32, make_plan, near16, operands, bits8
 
 pytestmark = pytest.mark.gpu
 
@@ -202,6 +202,37 @@ def test_an_experts_rows_are_those_of_the_plain_product():
             one = torch.zeros(m, n, dtype=BF16, device="cuda")
             sx.gemm_f8(xc[a:a + m].cuda(), xs[a:a + m].cuda(), wc[e].cuda(), ws[e].cuda(), one)
             assert torch.equal(one.cpu(), y[a:a + m]), f"expert {e}"
+
+
+@pytest.mark.parametrize("e,places,n,k,even", [
+    (16, 250, 1024, 512, False), (128, 6000, 2176, 768, True), (4, 6800, 1280, 256, False), (32, 7200, 1152, 256, True),
+    (4, 1280, 7040, 256, False), (4, 3000, 2176, 1664, False), (8, 160, 7552, 128, False), (64, 6040, 2048, 512, False),
+    (8, 8000, 4224, 512, False), (16, 5050, 2048, 256, False), (8, 7100, 5504, 128, False), (1100, 2000, 128, 128, False),
+    (6, 4000, 2176, 16512, False), (2, 40, 128, 40064, True),
+])
+def test_large_grouped_launches(e, places, n, k, even):
+    # the bits of gemm_f8, expert by expert, under a list of places and where each goes
+    g = gen(places + n)
+    counts = torch.bincount(torch.arange(places) % e if even else (torch.rand(places, generator=g) ** 2 * e).long(), minlength=e)
+    off = torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)]).int()
+    made = [codes(g, 0, k, n) for _ in range(min(e, 16))]
+    wc, ws = (torch.stack([made[i % 16][j] for i in range(e)]) for j in (0, 1))
+    x, xs = codes(g, places, k)
+    order = torch.randperm(places, generator=g).int().cuda()
+    y = torch.full((places + 3, n), 7.0, dtype=BF16, device="cuda")
+    sx.gemm_experts_f8(x, xs, wc, ws, off.cuda(), torch.cat([order, order[:3]]), y, gather=1)
+    z = torch.full((places + 3, n), 7.0, dtype=BF16, device="cuda")
+    sx.gemm_experts_f8(x, xs, wc, ws, off.cuda(), torch.cat([order, order[:3]]), z, scatter=True)
+    assert (y[places:] == 7).all() and (z[places:] == 7).all()
+    for i in range(e):
+        a, b = int(off[i]), int(off[i + 1])
+        if a < b:
+            p = order[a:b].long()
+            one = torch.empty(b - a, n, dtype=BF16, device="cuda")
+            sx.gemm_f8(x[p], xs[p], *made[i % 16], one)
+            assert torch.equal(y[a:b], one), f"gather, expert {i}"
+            sx.gemm_f8(x[a:b], xs[a:b].clone(), *made[i % 16], one)
+            assert torch.equal(z[p], one), f"scatter, expert {i}"
 
 
 # ---------------------------------------------------------------- the weighted sum
