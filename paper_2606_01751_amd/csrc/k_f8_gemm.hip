@@ -445,6 +445,7 @@ struct Feed {
   }
   __device__ __forceinline__ static i32x4_t lds16(uint32_t at) { return *(const __attribute__((address_space(3))) i32x4_t*)(uintptr_t)at; }
   __device__ __forceinline__ static int lds1(uint32_t at) { return (int)*(const __attribute__((address_space(3))) uint8_t*)(uintptr_t)at; }
+  __device__ __forceinline__ static int lds4(uint32_t at) { return *(const __attribute__((address_space(3))) int*)(uintptr_t)at; }
   __device__ __forceinline__ int w_scale(int tile, int b) const { return lds1(ws_at + min(tile, tiles - 1) * tile_w_scales(BN, a.ld) + b); }
   __device__ __forceinline__ int x_scale(int b, int j) const { return lds1(xs_at + (b >> 2) * (4 * BM) + (b & 3) + j * 64); }
 };
@@ -573,13 +574,13 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
   }
 }
 
-// Small tiles: a wave's few matrix instructions a block do not cover the way of its operands from LDS, so KB blocks are
-// taken at once, with one barrier (KB > 1: of a single tile).  NST is the number of blocks that LDS holds.
-template <int BN, int BM, int WN, int WM, int KB, int NST, bool EXPERTS>
-__global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
+// Tiles of which two workgroups share a compute unit and fill each other's waits: a block is read, the next one's transfers
+// go out, the block's matrix instructions run.
+template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
+__global__ __launch_bounds__(WN * WM * 64, 1) void f8_pair_kernel(F8GemmK a) {
   typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
   constexpr int FI = F::FI, RJ = F::RJ, ND = F::ND, STAGE = F::STAGE;
-  static_assert(NST % KB == 0 && NST > KB && NST * ND < 64, "transfers in flight");
+  static_assert(NST > 1 && NST * ND < 64, "transfers in flight");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   F f(a, threadIdx.x);
   Place fill;
@@ -595,8 +596,8 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(f.lr * kF8Group + (chunk_swz(4 * h + f.g, f.lr) << 4));
   f32x4_t acc[FI][RJ];
-  i32x8_t fw[KB][FI], fx[KB][RJ];
-  int sw[KB], sx[KB][RJ];
+  i32x8_t fw[FI], fx[RJ];
+  int sw, sx[RJ];
   auto read = [&](uint32_t base) { return operand(F::lds16(base + lane_off[0]), F::lds16(base + lane_off[1])); };
   const uint32_t wb = f.lds0 + (uint32_t)(f.wn * FI * 16 * kF8Group), xb = f.lds0 + (uint32_t)((BN + f.wm * RJ * 16) * kF8Group);
   bool first = true;
@@ -605,49 +606,119 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
     for (int i = 0; i < FI; ++i)
 #pragma unroll
       for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
-    for (int b = 0; b < f.nb; b += KB) {
-      // the KB blocks have landed: all transfers but those of the NST - 2 KB (at first NST - KB) blocks behind them, and all
-      // waves have read the KB before, whose stages are refilled
-      if (first) SX_WAIT_VM((NST - KB) * ND & 63);
-      else SX_WAIT_VM((NST - 2 * KB) * ND & 63);
+    for (int b = 0; b < f.nb; ++b) {
+      // the block has landed: all transfers but those of the NST - 2 (at first NST - 1) blocks behind it, and all waves have
+      // read the block before, whose stage is refilled
+      if (first) SX_WAIT_VM((NST - 1) * ND & 63);
+      else SX_WAIT_VM((NST - 2) * ND & 63);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __syncthreads();
+      const uint32_t at = (uint32_t)(stage * STAGE);
+      sw = f.w_scale(tile, b);
 #pragma unroll
-      for (int s = 0; s < KB; ++s) {
-        const uint32_t at = (uint32_t)(stage * STAGE);
-        const int c = min(b + s, f.nb - 1);   // (what is read behind the last block is never used)
-        sw[s] = f.w_scale(tile, c);
+      for (int j = 0; j < RJ; ++j) sx[j] = f.x_scale(b, j);
 #pragma unroll
-        for (int j = 0; j < RJ; ++j) sx[s][j] = f.x_scale(c, j);
+      for (int i = 0; i < FI; ++i) {
+        fw[i] = read(wb + at + (uint32_t)(i * 16 * kF8Group));
+        if (i == 0)
 #pragma unroll
-        for (int i = 0; i < FI; ++i) {
-          fw[s][i] = read(wb + at + (uint32_t)(i * 16 * kF8Group));
-          if (i == 0)
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) fx[s][j] = read(xb + at + (uint32_t)(j * 16 * kF8Group));
-        }
-        stage = stage + 1 == NST ? 0 : stage + 1;
+          for (int j = 0; j < RJ; ++j) fx[j] = read(xb + at + (uint32_t)(j * 16 * kF8Group));
       }
-      if (!first)
+      stage = stage + 1 == NST ? 0 : stage + 1;
+      if (!first) {
 #pragma unroll
-        for (int s = 0; s < KB; ++s) {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) f.dma(fill, d);
-          f.advance(fill);
-        }
+        for (int d = 0; d < ND; ++d) f.dma(fill, d);
+        f.advance(fill);
+      }
       first = false;
 #pragma unroll
-      for (int s = 0; s < KB; ++s)
-        if (b + s < f.nb)
+      for (int i = 0; i < FI; ++i)
 #pragma unroll
-          for (int i = 0; i < FI; ++i)
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) acc[i][j] = mfma_block<0>(fw[s][i], fx[s][j], acc[i][j], sw[s], sx[s][j]);
+        for (int j = 0; j < RJ; ++j) acc[i][j] = mfma_block<0>(fw[i], fx[j], acc[i][j], sw, sx[j]);
     }
     const int nw = f.n0 + tile * BN + f.wn * (BN / WN);
     if (a.run == 1) __syncthreads();   // (all waves have read the stages)
     if (nw < a.N) put_tile<false>(a, f.yrow, nw, acc, f.out, f.lane);
   }
+}
+
+// Small tiles: a wave's few matrix instructions a block do not cover the way of its operands from LDS, so those of the next
+// block are read, into a second set of registers, before the block's matrix instructions and transfers.  One tile a
+// workgroup.  The bound is LDS, which takes a transfer's kilobyte in 21 cycles and reads at 128 bytes a cycle: of a block's
+// 420 cycles in 64 x 32 tiles 252 and 192 (96 rows x 4096 x 14336; without the reads 340, without the transfers 180).
+template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
+__global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
+  typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
+  constexpr int FI = F::FI, RJ = F::RJ, ND = F::ND, STAGE = F::STAGE;
+  static_assert(NST > 2 && NST * ND < 64, "transfers in flight");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  F f(a, threadIdx.x);
+  Place fill;
+  if (!f.start(smem, &fill)) return;
+#pragma unroll
+  for (int b = 0; b < NST; ++b) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) f.dma(fill, d);
+    f.advance(fill);
+  }
+  uint32_t lane_off[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) lane_off[h] = (uint32_t)(f.lr * kF8Group + (chunk_swz(4 * h + f.g, f.lr) << 4));
+  f32x4_t acc[FI][RJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4_t{};
+  i32x8_t fw[2][FI], fx[2][RJ];
+  int sw, sx[RJ], swn = 0, sxn[RJ] = {};
+  const uint32_t wb = f.lds0 + (uint32_t)(f.wn * FI * 16 * kF8Group), xb = f.lds0 + (uint32_t)((BN + f.wm * RJ * 16) * kF8Group);
+  uint32_t at = 0;   // the stage of the next block that is read
+  auto read_at = [&](uint32_t base) { return operand(F::lds16(base + lane_off[0]), F::lds16(base + lane_off[1])); };
+  auto read = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FI; ++i) fw[s][i] = read_at(wb + at + (uint32_t)(i * 16 * kF8Group));
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) fx[s][j] = read_at(xb + at + (uint32_t)(j * 16 * kF8Group));
+    at = at + STAGE == NST * STAGE ? 0 : at + STAGE;
+  };
+  SX_WAIT_VM((NST - 1) * ND & 63);
+  __syncthreads();
+  read(0);
+  sw = F::lds4(f.ws_at);
+#pragma unroll
+  for (int j = 0; j < RJ; ++j) sx[j] = F::lds4(f.xs_at + j * 64);
+  auto step = [&](auto c, int b) __attribute__((always_inline)) {
+    constexpr int S = decltype(c)::value;
+    if (b + S >= f.nb) return;
+    __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (0x7 << 4));   // lgkmcnt 0: this block's operands
+    SX_WAIT_VM((NST - 2) * ND & 63);                            // the next block has landed
+    __syncthreads();
+    read((S + 1) % 2);
+    if (S == 3) {
+      const int q = min(b + 4, f.nb - 1) & ~3;
+      swn = F::lds4(f.ws_at + q);
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) sxn[j] = F::lds4(f.xs_at + q * BM + j * 64);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < max(FI * RJ, ND); ++m) {
+      if (m < ND) f.dma(fill, m);
+      if (m < FI * RJ) acc[m % FI][m / FI] = mfma_block<S>(fw[S % 2][m % FI], fx[S % 2][m / FI], acc[m % FI][m / FI], sw, sx[m / FI]);
+    }
+    f.advance(fill);
+    if (S == 3) {
+      sw = swn;
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) sx[j] = sxn[j];
+    }
+  };
+  for (int b = 0; b < f.nb; b += 4)
+    [&]<int... S>(std::integer_sequence<int, S...>) { (step(std::integral_constant<int, S>{}, b), ...); }(std::make_integer_sequence<int, 4>{});
+  const int nw = f.n0 + f.wn * (BN / WN);
+  __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (0x7 << 4));
+  __syncthreads();   // (all waves have read the stages)
+  if (nw < a.N) put_tile<false>(a, f.yrow, nw, acc, f.out, f.lane);
 }
 
 // Row tiles of BM rows that the launch may have to take.
@@ -691,8 +762,9 @@ hipError_t launch_tiled(F8GemmK& a, int n_cu, int most, hipStream_t s, K plain, 
       lds = need;
     }
   }
+  if (lds == 0) return hipErrorInvalidConfiguration;
   const int64_t blocks = (m_tiles * ((n_tiles + a.run - 1) / a.run) + kXcds - 1) / kXcds * kXcds;
-  if (lds == 0 || blocks >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
+  if (blocks >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(a.offsets ? experts : plain, dim3((unsigned)blocks), dim3(WN * WM * 64), lds, s, a);
   return hipGetLastError();
 }
@@ -701,49 +773,55 @@ hipError_t launch_tile(F8GemmK& a, int n_cu, hipStream_t s) {
   return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, kRun, s, f8_tile_kernel<BN, BM, WN, WM, NST, false>,
                                            f8_tile_kernel<BN, BM, WN, WM, NST, true>);
 }
-template <int BN, int BM, int WN, int WM, int KB, int NST>
+template <int BN, int BM, int WN, int WM, int NST>
+hipError_t launch_pair(F8GemmK& a, int n_cu, hipStream_t s) {
+  return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, kRun, s, f8_pair_kernel<BN, BM, WN, WM, NST, false>,
+                                           f8_pair_kernel<BN, BM, WN, WM, NST, true>);
+}
+template <int BN, int BM, int WN, int WM, int NST>
 hipError_t launch_narrow(F8GemmK& a, int n_cu, hipStream_t s) {
-  return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, KB == 1 ? kRun : 1, s, f8_narrow_kernel<BN, BM, WN, WM, KB, NST, false>,
-                                           f8_narrow_kernel<BN, BM, WN, WM, KB, NST, true>);
+  return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, 1, s, f8_narrow_kernel<BN, BM, WN, WM, NST, false>,
+                                           f8_narrow_kernel<BN, BM, WN, WM, NST, true>);
 }
 
-// What a launch of a shape takes, fitted to 90 products of 1 to 6712 rows by six weights of 768 to 14336 x 1024 to 28672 and
-// 26 grouped ones: `first` us and `block` us a block of k for a first round of workgroups, occ on each compute unit,
+// What a launch of a shape takes, fitted to 105 products of 1 to 6712 rows by seven weights of 768 to 14336 x 1024 to 28672,
+// weights from memory: `first` us and `block` us a block of k for a first round of workgroups, occ on each compute unit,
 // `more` and `more_block` for each further one.
 struct Shape {
   int bn, bm, nst, occ;
   double first, block, more, more_block;
 };
-enum { kStream, k16x16, k64x32, k64x64, k128x64, k128x128, k128x128x2, k256x256, kShapes };
-constexpr Shape kShape[kShapes] = {{16, 16, 0, 1, 2.42, 0.124, 0.01, 0.114}, {16, 16, 12, 3, 4.04, 0.206, 2.95, 0.204},
-                                   {64, 32, 10, 1, 4.01, 0.234, 2.76, 0.230}, {64, 64, 6, 1, 3.75, 0.281, 2.65, 0.281},
-                                   {128, 64, 3, 1, 3.40, 0.396, 1.30, 0.316}, {128, 128, 4, 1, 4.06, 0.561, 1.44, 0.605},
-                                   {128, 128, 2, 2, 1.98, 0.808, 5.66, 1.067}, {256, 256, 2, 1, 8.42, 1.240, 4.26, 1.571}};
+enum { kStream, k32x32, k64x32, k64x64, k128x64, k128x128, k128x128x2, k256x256, kShapes };
+constexpr Shape kShape[kShapes] = {{16, 16, 0, 1, 2.70, 0.155, 0.03, 0.113}, {32, 32, 6, 1, 3.68, 0.193, 0.84, 0.093},
+                                   {64, 32, 6, 1, 3.71, 0.220, 1.26, 0.148}, {64, 64, 4, 1, 3.62, 0.294, 1.45, 0.200},
+                                   {128, 64, 3, 1, 3.19, 0.474, 2.09, 0.310}, {128, 128, 4, 1, 4.42, 0.554, 4.38, 0.591},
+                                   {128, 128, 2, 2, 3.00, 1.040, 9.23, 0.973}, {256, 256, 2, 1, 7.90, 1.414, 10.69, 1.437}};
 constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for grouped rows (of listed ones: 16)
 
-// The shape of least time: within 8% of the fastest for each of those 90 products (0.4% in the mean), within 13% for the
-// grouped ones (2.4%).  Some of them in us, the shape taken and its neighbours in the table: K = 4096, 1 row x 4096 features
-// 7.0 (10.3), 16 x 6144 10.4 (10.9, 11.4), 96 x 4096 11.7 (22.8, 12.8), 200 x 4096 13.2 (21.5, 15.9), 394 x 4096 16.2 (24.0,
-// 21.7), 1000 x 4096 22.8 (25.0, 28.4), 2048 x 4096 35.4 (41.2, 48.5), 6712 x 28672 631 (845); grouped, 2048 -> 3072, 64 tokens x
-// 8 of 128 experts 126 (130), 512 x 8 of 128 194 (217), 2048 x 2 of 8 42 (49, 59), 8192 x 8 of 128 560 (671).
+// The shape of least time; for those 105 products within 4% of the fastest (0.1% in the mean).  Some of them in us, the shape
+// taken and its neighbours in the table: K = 4096, 1 row x 4096 features 8.8 (9.9), 17 x 6144 10.2 (13.7, 10.9), 64 x 6144 11.8
+// (13.9, 14.2), 200 x 4096 13.2 (16.3, 18.1), 394 x 4096 18.5 (19.7, 22.2), 1000 x 4096 25.2 (28.8, 37.2), 2048 x 4096 43 (48, 60),
+// 6712 x 28672 669 (881).
+// Grouped rows: few for each expert, by the streaming kernel, since the weights' way from memory is the bound (64 tokens x 8
+// of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, 2048 -> 3072: 185, 166); else by the same costs and as
+// many tiles as rows spread over the experts make, each expert's last one half full (2048 -> 3072: 512 x 8 of 128 193 us of
+// 128 x 64, 213 of 128 x 128; 2048 x 2 of 8 42 of 128 x 128, 48 of 128 x 64, 60 of 256 x 256; 8192 x 8 of 128 574 of 256 x 256, 688 of
+// 128 x 128; of 26 such products within 7% of the fastest but for five, which are 9 to 20% off).
 int best_shape(const F8GemmK& a, int n_cu) {
+  const bool ex = a.offsets;
+  if (ex && a.n_places <= 12 * (int64_t)a.n_experts) return kStream;
   int best = kStream;
   double least = 1e300;
   const double nb = a.K / kF8Group;
-  for (int i = 0; i < kShapes; ++i) {
+  for (int i = ex ? k128x64 : kStream; i < kShapes; ++i) {
     const Shape& h = kShape[i];
-    const bool ex = a.offsets, stream = i == kStream;
-    const int bn = ex && stream ? kStreamExperts : h.bn, bm = ex && stream ? kStreamExperts : h.bm;
-    if (ex && (i == k16x16 || i == k64x32 || i == k64x64)) continue;   // (no grouped product measured faster by one)
-    const int64_t n_tiles = (a.N + bn - 1) / bn, most = count_tiles(a, bm) * n_tiles;
-    if ((!stream && (a.ld > kLdsBytes / bm || tile_fixed(bn, bm, h.nst, a.ld, 1) > kLdsBytes)) || most >= ((int64_t)1 << 31) - 64) continue;
+    const int64_t n_tiles = (a.N + h.bn - 1) / h.bn, most = count_tiles(a, h.bm) * n_tiles;
+    if ((h.nst && (a.ld > kLdsBytes / h.bm || tile_fixed(h.bn, h.bm, h.nst, a.ld, 1) > kLdsBytes)) || most >= ((int64_t)1 << 31) - 64)
+      continue;
     double tiles = (double)most;
-    if (ex) {   // as many as rows spread over the experts make, each expert's last one half full
-      const double groups = a.n_places < a.n_experts ? a.n_places : a.n_experts, full = a.n_places / groups / bm;
-      tiles = groups * (full > 0.5 ? full + 0.5 : 1) * (double)n_tiles + n_cu / 8;
-      // Few rows an expert: the weights' way from memory is the bound, which the streaming kernel comes nearest to (64 tokens
-      // x 8 of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, 2048 -> 3072: 184, 166).
-      if (stream && a.n_places <= 12 * (int64_t)a.n_experts) return kStream;
+    if (ex) {
+      const double full = (double)a.n_places / a.n_experts / h.bm;
+      tiles = a.n_experts * (full > 0.5 ? full + 0.5 : 1) * (double)n_tiles + n_cu / 8;
     }
     const double rounds = ceil(tiles / ((double)n_cu * h.occ));
     const double t = h.first + nb * h.block + (rounds - 1) * (h.more + nb * h.more_block);
@@ -760,12 +838,12 @@ int best_shape(const F8GemmK& a, int n_cu) {
 hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
   switch (best_shape(a, n_cu)) {
     case kStream: return a.offsets ? launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4>(a, s) : launch_stream<1, 1, 8>(a, s);
-    case k16x16: return launch_narrow<16, 16, 1, 1, 4, 12>(a, n_cu, s);
-    case k64x32: return launch_narrow<64, 32, 4, 1, 2, 10>(a, n_cu, s);
-    case k64x64: return launch_narrow<64, 64, 2, 2, 2, 6>(a, n_cu, s);
-    case k128x64: return launch_narrow<128, 64, 4, 2, 1, 3>(a, n_cu, s);
-    case k128x128: return launch_narrow<128, 128, 4, 2, 1, 4>(a, n_cu, s);
-    case k128x128x2: return launch_narrow<128, 128, 4, 2, 1, 2>(a, n_cu, s);
+    case k32x32: return launch_narrow<32, 32, 2, 2, 6>(a, n_cu, s);
+    case k64x32: return launch_narrow<64, 32, 2, 2, 6>(a, n_cu, s);
+    case k64x64: return launch_narrow<64, 64, 2, 2, 4>(a, n_cu, s);
+    case k128x64: return launch_narrow<128, 64, 4, 2, 3>(a, n_cu, s);
+    case k128x128: return launch_narrow<128, 128, 4, 2, 4>(a, n_cu, s);
+    case k128x128x2: return launch_pair<128, 128, 4, 2, 2>(a, n_cu, s);
     default: return launch_tile<256, 256, 2, 2, 2>(a, n_cu, s);
   }
 }

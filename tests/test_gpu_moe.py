@@ -208,7 +208,8 @@ def test_an_experts_rows_are_those_of_the_plain_product():
     (16, 250, 1024, 512, False), (128, 6000, 2176, 768, True), (4, 6800, 1280, 256, False), (32, 7200, 1152, 256, True),
     (4, 1280, 7040, 256, False), (4, 3000, 2176, 1664, False), (8, 160, 7552, 128, False), (64, 6040, 2048, 512, False),
     (8, 8000, 4224, 512, False), (16, 5050, 2048, 256, False), (8, 7100, 5504, 128, False), (1100, 2000, 128, 128, False),
-    (6, 4000, 2176, 16512, False), (2, 40, 128, 40064, True),
+    (6, 4000, 2176, 16512, False), (2, 40, 128, 40064, True), (64, 8000, 1920, 128, True), (8, 128, 7296, 128, True),
+    (4, 1200, 1408, 512, False), (4, 70, 384, 1152, False),
 ])
 def test_large_grouped_launches(e, places, n, k, even):
     # the bits of gemm_f8, expert by expert, under a list of places and where each goes
