@@ -18,7 +18,7 @@
  *
  * Status, streams, memory ownership and sx_last_error are as in include/sx.h: no call allocates,
  * synchronises the host, aborts or throws; every tensor is caller-owned DEVICE memory on the current
- * device, 16-byte aligned where it holds elements.  Nothing is kept between calls: calls may run at the
+ * device, 16-byte aligned but for rows and n_rows (4 bytes).  Nothing is kept between calls: calls may run at the
  * same time on any streams when their outputs and workspaces differ, and any of them can be captured into
  * a graph.  An output must not overlap another argument of its call (SX_EINVAL) but where this says so.
  * Index arrays in device memory are trusted by the release library, but an entry that is out of range is

@@ -723,15 +723,14 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
 
 // Row tiles of BM rows that the launch may have to take.
 int64_t count_tiles(const F8GemmK& a, int bm) {
-  if (!a.offsets) return (int64_t)a.r.n_req * ((a.r.max_rows + bm - 1) / bm);
+  if (!a.offsets) return (int64_t)a.r.n_req * (((int64_t)a.r.max_rows + bm - 1) / bm);
   return a.n_places / bm + (int64_t)(a.n_experts < a.n_places ? a.n_experts : a.n_places);
 }
 
 template <int FI, int RJ, int D>
 hipError_t launch_stream(F8GemmK& a, hipStream_t s) {
-  a.m_tiles = (a.r.max_rows + 16 * RJ - 1) / (16 * RJ);
+  a.m_tiles = (int)(((int64_t)a.r.max_rows + 16 * RJ - 1) / (16 * RJ));
   const int64_t blocks = count_tiles(a, 16 * RJ) * (a.N / (16 * FI));
-  if (blocks >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   if (a.offsets)
     hipLaunchKernelGGL((f8_stream_kernel<FI, RJ, D, true>), dim3((unsigned)blocks), dim3(64), 0, s, a);
   else
@@ -747,7 +746,7 @@ constexpr int kRun = 4;
 template <int BN, int BM, int WN, int WM, int NST, typename K>
 hipError_t launch_tiled(F8GemmK& a, int n_cu, int most, hipStream_t s, K plain, K experts) {
   const int64_t m_tiles = count_tiles(a, BM), n_tiles = (a.N + BN - 1) / BN;
-  a.m_tiles = a.offsets ? (int)m_tiles : (a.r.max_rows + BM - 1) / BM;
+  a.m_tiles = a.offsets ? (int)m_tiles : (int)(((int64_t)a.r.max_rows + BM - 1) / BM);
   constexpr int kOut = WN * WM * epilogue_lds<BN / WN / 16>();
   int lds = 0;
   int64_t least = INT64_MAX;
@@ -764,7 +763,6 @@ hipError_t launch_tiled(F8GemmK& a, int n_cu, int most, hipStream_t s, K plain, 
   }
   if (lds == 0) return hipErrorInvalidConfiguration;
   const int64_t blocks = (m_tiles * ((n_tiles + a.run - 1) / a.run) + kXcds - 1) / kXcds * kXcds;
-  if (blocks >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(a.offsets ? experts : plain, dim3((unsigned)blocks), dim3(WN * WM * 64), lds, s, a);
   return hipGetLastError();
 }
@@ -788,14 +786,16 @@ hipError_t launch_narrow(F8GemmK& a, int n_cu, hipStream_t s) {
 // weights from memory: `first` us and `block` us a block of k for a first round of workgroups, occ on each compute unit,
 // `more` and `more_block` for each further one.
 struct Shape {
-  int bn, bm, nst, occ;
+  int bn, bm, nst, threads, occ;
   double first, block, more, more_block;
 };
 enum { kStream, k32x32, k64x32, k64x64, k128x64, k128x128, k128x128x2, k256x256, kShapes };
-constexpr Shape kShape[kShapes] = {{16, 16, 0, 1, 2.70, 0.155, 0.03, 0.113}, {32, 32, 6, 1, 3.68, 0.193, 0.84, 0.093},
-                                   {64, 32, 6, 1, 3.71, 0.220, 1.26, 0.148}, {64, 64, 4, 1, 3.62, 0.294, 1.45, 0.200},
-                                   {128, 64, 3, 1, 3.19, 0.474, 2.09, 0.310}, {128, 128, 4, 1, 4.42, 0.554, 4.38, 0.591},
-                                   {128, 128, 2, 2, 3.00, 1.040, 9.23, 0.973}, {256, 256, 2, 1, 7.90, 1.414, 10.69, 1.437}};
+constexpr Shape kShape[kShapes] = {
+    {16, 16, 0, 64, 1, 2.70, 0.155, 0.03, 0.113},    {32, 32, 6, 256, 1, 3.68, 0.193, 0.84, 0.093},
+    {64, 32, 6, 256, 1, 3.71, 0.220, 1.26, 0.148},   {64, 64, 4, 256, 1, 3.62, 0.294, 1.45, 0.200},
+    {128, 64, 3, 512, 1, 3.19, 0.474, 2.09, 0.310},  {128, 128, 4, 512, 1, 4.42, 0.554, 4.38, 0.591},
+    {128, 128, 2, 512, 2, 3.00, 1.040, 9.23, 0.973}, {256, 256, 2, 256, 1, 7.90, 1.414, 10.69, 1.437}};
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 4096;   // of a launch (and room for the grid's rounding)
 constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for grouped rows (of listed ones: 16)
 
 // The shape of least time; for those 105 products within 4% of the fastest (0.1% in the mean).  Some of them in us, the shape
@@ -809,14 +809,15 @@ constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for gr
 // 128 x 128; of 26 such products within 7% of the fastest but for five, which are 9 to 20% off).
 int best_shape(const F8GemmK& a, int n_cu) {
   const bool ex = a.offsets;
-  if (ex && a.n_places <= 12 * (int64_t)a.n_experts) return kStream;
-  int best = kStream;
+  if (ex && a.n_places <= 12 * (int64_t)a.n_experts && count_tiles(a, kStreamExperts) * (a.N / kStreamExperts) * 64 < kMaxThreads)
+    return kStream;
+  int best = -1;
   double least = 1e300;
   const double nb = a.K / kF8Group;
   for (int i = ex ? k128x64 : kStream; i < kShapes; ++i) {
     const Shape& h = kShape[i];
     const int64_t n_tiles = (a.N + h.bn - 1) / h.bn, most = count_tiles(a, h.bm) * n_tiles;
-    if ((h.nst && (a.ld > kLdsBytes / h.bm || tile_fixed(h.bn, h.bm, h.nst, a.ld, 1) > kLdsBytes)) || most >= ((int64_t)1 << 31) - 64)
+    if ((h.nst && (a.ld > kLdsBytes / h.bm || tile_fixed(h.bn, h.bm, h.nst, a.ld, 1) > kLdsBytes)) || most * h.threads >= kMaxThreads)
       continue;
     double tiles = (double)most;
     if (ex) {
@@ -844,7 +845,8 @@ hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
     case k128x64: return launch_narrow<128, 64, 4, 2, 3>(a, n_cu, s);
     case k128x128: return launch_narrow<128, 128, 4, 2, 4>(a, n_cu, s);
     case k128x128x2: return launch_pair<128, 128, 4, 2, 2>(a, n_cu, s);
-    default: return launch_tile<256, 256, 2, 2, 2>(a, n_cu, s);
+    case k256x256: return launch_tile<256, 256, 2, 2, 2>(a, n_cu, s);
+    default: return hipErrorInvalidConfiguration;   // (more workgroups than a launch has)
   }
 }
 

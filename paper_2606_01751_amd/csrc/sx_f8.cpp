@@ -16,7 +16,6 @@ using sx::aligned16;
 using sx::overlap;
 using sx::reportf;
 
-constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - ((int64_t)1 << 16);   // of a one-dimensional launch
 constexpr int kMaxRequests = 65535;
 
@@ -88,6 +87,13 @@ sx_status rows_of(const char* who, const sx_plan* p, const int32_t* rows, const 
   return sx::check_row_list(p, rows, n_rows, max_rows, stream, who);
 }
 
+sx_status gemm_launch(const char* who, sx::F8GemmK& a, int rows, int64_t n, const char* what, void* stream) {
+  const hipError_t e = sx::launch_gemm_f8(a, sx::cu_count(), (hipStream_t)stream);
+  if (e == hipErrorInvalidConfiguration)
+    return reportf(SX_EUNSUPPORTED, "%s: %d rows x %lld features exceed one launch", who, rows, (long long)n);
+  return sx::launch_status(e, what);
+}
+
 Arg n_rows_arg(const sx_plan* p, const int32_t* n_rows) { return {n_rows, 4ll * (p ? p->n_req : 1), "n_rows"}; }
 Arg rows_arg(const sx_plan* p, const int32_t* rows) { return {rows, p ? 4 * p->total : 0, "rows"}; }
 
@@ -106,9 +112,9 @@ sx_status sx_f8_scale_ld(int32_t k, int32_t* ld) {
 sx_status sx_f8_pack_weight(const void* w, int64_t n, int32_t k, void* codes, void* scales, void* stream) {
   const char* who = "sx_f8_pack_weight";
   if (n == 0) return SX_OK;
-  sx_status st = width_ok(who, "n", n, (int64_t)1 << 40);
+  sx_status st = width_ok(who, "n", n, (int64_t)1 << 36);
   if (st != SX_OK) return st;
-  if ((st = width_ok(who, "k", k, INT32_MAX)) != SX_OK) return st;
+  if ((st = width_ok(who, "k", k, 1 << 24)) != SX_OK) return st;
   if (!w || !codes || !scales) return reportf(SX_EINVAL, "%s: NULL argument", who);
   const Arg in[] = {{w, 2 * n * k, "w"}}, out[] = {{codes, n * k, "codes"}, {scales, n / sx::kF8Group * sx::f8_ld(k), "scales"}};
   if ((st = aligned(who, in)) != SX_OK || (st = aligned(who, out)) != SX_OK) return st;
@@ -226,10 +232,7 @@ sx_status sx_gemm_f8(const sx_plan* plan, const int32_t* rows, const int32_t* n_
   a.res = (const uint16_t*)residual;
   a.x_tok = x_by_token != 0;
   a.y_tok = y_by_token != 0;
-  // (the smallest tile of the launches: 16 rows x 16 features)
-  if (((int64_t)max_rows + 15) / 16 * a.r.n_req * (n / 16) > kMaxGrid)
-    return reportf(SX_EUNSUPPORTED, "%s: %d rows x %lld features exceed one launch", who, max_rows, (long long)n);
-  return sx::launch_status(sx::launch_gemm_f8(a, sx::cu_count(), (hipStream_t)stream), "sx_gemm_f8 launch");
+  return gemm_launch(who, a, max_rows, n, "sx_gemm_f8 launch", stream);
 }
 
 sx_status sx_moe_route_workspace(int32_t n_experts, int32_t top_k, int32_t n_requests, int32_t max_rows, int64_t* bytes) {
@@ -326,9 +329,7 @@ sx_status sx_gemm_experts_f8(const int32_t* offsets, const int32_t* order, int32
   a.x_rows = x_rows;
   a.gather = gather;
   a.scatter = scatter != 0;
-  if ((rows / 16 + std::min<int64_t>(n_experts, rows)) * (n / 16) > kMaxGrid)
-    return reportf(SX_EUNSUPPORTED, "%s: %d places x %d features exceed one launch", who, n_places, n);
-  return sx::launch_status(sx::launch_gemm_f8(a, sx::cu_count(), (hipStream_t)stream), "sx_gemm_experts_f8 launch");
+  return gemm_launch(who, a, n_places, n, "sx_gemm_experts_f8 launch", stream);
 }
 
 sx_status sx_moe_combine(const sx_plan* plan, const int32_t* rows, const int32_t* n_rows, int32_t max_rows,

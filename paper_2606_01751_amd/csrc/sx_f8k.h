@@ -70,7 +70,6 @@ struct MoeRouteK {
   int32_t* counts;   // [blocks][n_experts]
   int n_experts, top_k, renormalise;
   int blocks, per_req, rows_per_block, reqs_per_block;   // see moe_blocks
-  int64_t slots;     // of logits, ids and weights
 };
 
 struct MoeCombineK {
@@ -110,7 +109,7 @@ hipError_t device_check_order(const int32_t* offsets, int32_t n_experts, const i
 hipError_t launch_f8_pack_weight(const uint16_t* w, int64_t n, int k, uint8_t* codes, uint8_t* scales, hipStream_t s);
 hipError_t launch_add_rmsnorm_f8(const F8NormK& a, hipStream_t s);
 hipError_t launch_silu_mul_f8(const F8SiluK& a, hipStream_t s);
-hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s);
+hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s);   // hipErrorInvalidConfiguration: too many tiles
 hipError_t launch_moe_route(const MoeRouteK& a, bool f32, hipStream_t s);
 hipError_t launch_moe_combine(const MoeCombineK& a, hipStream_t s);
 

@@ -78,13 +78,16 @@ def _like(t, rows: int, width: int, at: int, what: str):
     return p
 
 
-def _index(t, n: int, at: int, what: str):
-    """Pointer of an int32 array of at least n entries; row lists of a plan come as pointers too."""
-    if t is None or isinstance(t, int):
-        return t
-    if t.numel() < n:
-        raise ValueError(f"{what} needs {n} entries")
+def _entries(t, n: int, at: int, what: str):
+    """Pointer of an int32 array of at least n entries."""
+    if not isinstance(t, torch.Tensor) or t.numel() < n:
+        raise ValueError(f"{what} must be an int32 tensor of {n} entries")
     return _ptr(t, _I32, at, what)
+
+
+def _index(t, n: int, at: int, what: str):
+    """The same; row lists of a plan come as pointers too."""
+    return t if t is None or isinstance(t, int) else _entries(t, n, at, what)
 
 
 def _row_args(plan, rows, n_rows, max_rows, have: int, at: int):
@@ -93,7 +96,7 @@ def _row_args(plan, rows, n_rows, max_rows, have: int, at: int):
         _need(rows is None, "a row list needs a plan")
         n = _int(have if max_rows is None else max_rows, "max_rows")
         _need(n <= have, f"max_rows {n} exceeds the arrays' {have} rows")
-        return None, None, None if n_rows is None else _index(n_rows, 1, at, "n_rows"), n
+        return None, None, None if n_rows is None else _entries(n_rows, 1, at, "n_rows"), n
     info = plan.info()
     total = info["total_tokens"]
     _need(have == total, f"the arrays have {have} rows, the plan {total} tokens")
@@ -205,7 +208,7 @@ def gemm_experts_f8(x8, x_scale, w8, w_scale, offsets, order, y, gather: int = 0
     e = w8.shape[0]
     _need(offsets.numel() == e + 1, "offsets needs experts + 1 entries")
     _check(lib().sx_gemm_experts_f8(
-        _ptr(offsets, _I32, at, "offsets"), _index(order, places, at, "order"), e, _int(places, "places"), xp, xsp,
+        _ptr(offsets, _I32, at, "offsets"), None if order is None else _entries(order, places, at, "order"), e, _int(places, "places"), xp, xsp,
         _int(x_rows, "rows of x"), _int(gather, "gather"), _matrix(w8, _CODES, e * n, k, at, "w8"),
         _matrix(w_scale, _SCALES, e * (n // 128), _ld(k), at, "w_scale"), k, n, yp, int(bool(scatter)), _on(stream, at)))
 

@@ -140,6 +140,14 @@ def test_gemm_experts_f8_refusals(kw, want, text):
     err(experts(**kw), want, text)
 
 
+def test_products_of_more_workgroups_than_a_launch_has():
+    # a launch has fewer than 2^32 threads: 2^28 rows x 2^21 features are 2^33 tiles of 256 x 256
+    err(gemm(m=1 << 28, part_n=(1 << 20, 1 << 20), n=None, far=True), U, "one launch")
+    err(gemm(m=(1 << 31) - 1, part_n=(1 << 20, 1 << 20), n=None, far=True), U, "one launch")
+    err(experts(e=65536, places=1 << 30, xr=1 << 30, n=1 << 22, far=True), U, "one launch")
+    err(experts(e=65536, places=1 << 16, xr=1 << 16, n=1 << 24, far=True), U, "one launch")
+
+
 @pytest.mark.parametrize("kw,want,text", [
     (dict(top=0), U, "top_k"), (dict(top=17), U, "top_k"), (dict(h=12), U, "multiple of 8"), (dict(h=0), U, "multiple of 8"),
     (dict(y=None), V, "NULL"), (dict(wt=None), V, "NULL"), (dict(out=None), V, "NULL"), (dict(out=at(3, 16)), V, "overlaps residual"),
@@ -194,6 +202,14 @@ def test_binding_refuses_what_is_not_on_the_gpu():
 
 
 # ---- the references ----
+
+def test_binding_takes_no_number_for_a_count_or_an_order():
+    # a raw number would be read as an address
+    from paper_2606_01751_amd import layer8
+    for bad in (5, 5.0, [5], torch.zeros(0, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="int32 tensor"):
+            layer8._row_args(None, None, bad, None, 8, 0)
+
 
 def test_e4m3_reference_against_torch():
     codes = torch.arange(256, dtype=torch.int32).to(torch.uint8)
