@@ -393,6 +393,42 @@ def test_gemm_f8_rows_of_a_plan(x_tok, y_tok):
     plan.close()
 
 
+def test_gemm_f8_of_many_short_requests():
+    lengths = [3] * 300
+    counts = [(7 * i) % 4 for i in range(300)]
+    plan = make_plan(lengths)
+    rows, n_rows, where = row_lists(lengths, counts, 15)
+    g = gen(15)
+    xc, xs, wc, ws = operands(g, 900, 256, 384)
+    res = hidden(g, 900, 256)
+    y, = run_gemm(xc, xs, wc, ws, [256], res, plan=plan, rows=rows, n_rows=n_rows, max_rows=3, x_by_token=True, y_by_token=True)
+    tok = torch.tensor([t for _, t in where])
+    want, = run_gemm(xc[tok], xs[tok], wc, ws, [256], res[tok])
+    assert torch.equal(y[tok], want)
+    rest = torch.ones(900, dtype=torch.bool)
+    rest[tok] = False
+    assert (y[rest] == 7).all()
+    plan.close()
+
+
+def test_products_on_two_streams_at_once():
+    g = gen(16)
+    sets = []
+    for rows, n, k in ((700, 2048, 1152), (300, 1024, 4096)):
+        xc, xs = codes(g, rows, k)
+        wc, ws = codes(g, 0, k, n)
+        want = torch.empty(rows, n, dtype=BF16, device="cuda")
+        sx.gemm_f8(xc, xs, wc, ws, want)
+        sets.append((xc, xs, wc, ws, want, torch.empty_like(want), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for xc, xs, wc, ws, want, y, s in sets:
+            sx.gemm_f8(xc, xs, wc, ws, y, stream=s)
+    torch.cuda.synchronize()
+    for *_, want, y, _ in sets:
+        assert torch.equal(y, want)
+
+
 def test_gemm_f8_residual_in_place():
     g = gen(12)
     for rows in (9, 150):
