@@ -204,7 +204,8 @@ def test_add_rmsnorm_f8_in_place_and_rows_of_extremes():
 
 # ---------------------------------------------------------------- SwiGLU
 
-@pytest.mark.parametrize("n,f,live", [(1, 128, None), (3, 640, 2), (17, 768, None), (5, 14336, None), (130, 1536, 129), (2, 512, 0)])
+@pytest.mark.parametrize("n,f,live", [(1, 128, None), (3, 640, 2), (17, 768, None), (5, 14336, None), (130, 1536, 129), (2, 512, 0),
+                                     (22001, 1152, None), (70000, 384, 69990)])
 def test_silu_mul_f8(n, f, live):
     g = gen(n + f)
     x = (torch.randn(n, 2 * f, generator=g) * torch.exp(torch.randn(2 * f, generator=g))).to(BF16)
@@ -215,6 +216,26 @@ def test_silu_mul_f8(n, f, live):
     why = R.held(y.cpu()[:m], s.cpu()[:m], R.silu_mul(x[:m, :f].double(), x[:m, f:].double()), 2.0 ** -20)
     assert why is None, why
     assert (y.cpu()[m:] == 7).all() and (s.cpu()[m:] == 7).all()
+
+
+def test_silu_mul_f8_of_every_gate():
+    # every bfloat16 from 2^-100 to 80 in magnitude, in groups of like magnitude: 2^-20 of the value (as above)
+    bits = torch.arange(1 << 15, dtype=torch.int32)
+    v = (bits << 16).view(torch.float32)
+    v = v[(v >= 2.0 ** -100) & (v <= 80)]
+    v = v[:len(v) // 128 * 128]
+    x = torch.stack([torch.cat([v, torch.full_like(v, 1.5)]), torch.cat([-v, torch.full_like(v, -0.75)])]).to(BF16)
+    f = len(v)
+    y, s = torch.empty(2, f, dtype=torch.uint8, device="cuda"), torch.empty(2, R.ld(f), dtype=torch.uint8, device="cuda")
+    sx.silu_mul_f8(x.cuda(), y, s)
+    why = R.held(y.cpu(), s.cpu(), R.silu_mul(x[:, :f].double(), x[:, f:].double()), 2.0 ** -20)
+    assert why is None, why
+    # beyond: 0 where e^-g has no float32, the gate itself above
+    x = torch.tensor([[-90.0, -1e4, -3e38, 90.0, 1e4, 3e38] + [0.0] * 122 + [1.0] * 128], dtype=BF16)
+    y, s = torch.empty(1, 128, dtype=torch.uint8, device="cuda"), torch.empty(1, 4, dtype=torch.uint8, device="cuda")
+    sx.silu_mul_f8(x.cuda(), y, s)
+    got = R.rows_of(y.cpu(), s.cpu())[0]
+    assert (got[:5] == 0).all() and abs(got[5] / 3e38 - 1) < 2.0 ** -3
 
 
 def test_silu_mul_f8_rows_of_a_plan_and_infinities():
