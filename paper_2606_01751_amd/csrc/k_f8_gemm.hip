@@ -153,23 +153,33 @@ template <int FI>
 constexpr int epilogue_lds() { return 16 * (32 * FI + 16); }   // (16 bytes a row against bank conflicts)
 // AGPR: the sums are in accumulation registers; the empty asm keeps the compiler from fetching all of them at once.
 template <bool AGPR, bool RES, int FI, int RJ>
-__device__ __forceinline__ void put_rows(const F8GemmK& a, const int64_t* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
+__device__ __forceinline__ void put_rows(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
   constexpr int LD = 32 * FI + 16, CH = 2 * FI, RPI = 64 / CH, IT = (16 + RPI - 1) / RPI;   // 16-byte chunks of a row, rows an instruction
   static_assert(64 % CH == 0, "whole rows an instruction");
   const int lr = lane % 16, g = lane / 16;
   const int part = part_of(a, nw);
-  const int64_t ld = a.pn[part + 1] - a.pn[part];
+  const uint32_t ld = (uint32_t)(a.pn[part + 1] - a.pn[part]);
   const int col = nw - a.pn[part] + lane % CH * 8;
-  i32x4_t res[IT];
+  uint16_t* const to = a.y[part] + col;
+  const uint16_t* const from = a.res + col;
   auto row_of = [&](int j, int it) { return RPI > 16 && lane / CH >= 16 ? -1 : yrow[16 * j + it * RPI + lane / CH]; };
+  int row[2][IT];           // of rows j and j + 1
+  i32x4_t res[IT], q[IT];   // rows j's residual, rows j - 1's results
+  auto rows = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+    for (int it = 0; it < IT; ++it) row[j % 2][it] = row_of(j, it);
+  };
   auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int64_t y = row_of(j, it);
-      res[it] = y >= 0 ? *(const i32x4_t*)(a.res + y * ld + col) : i32x4_t{};
-    }
+    for (int it = 0; it < IT; ++it) res[it] = row[j % 2][it] >= 0 ? *(const i32x4_t*)(from + (uint64_t)(uint32_t)row[j % 2][it] * ld) : i32x4_t{};
   };
   char* const mine = lds + lane / CH * LD + lane % CH * 16;
+  auto store = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+    for (int it = 0; it < IT; ++it)
+      if (row[j % 2][it] >= 0) *(i32x4_t*)(to + (uint64_t)(uint32_t)row[j % 2][it] * ld) = q[it];
+  };
+  rows(0);
   if constexpr (RES) fetch(0);
 #pragma unroll
   for (int j = 0; j < RJ; ++j) {
@@ -177,35 +187,42 @@ __device__ __forceinline__ void put_rows(const F8GemmK& a, const int64_t* yrow, 
 #pragma unroll
       for (int it = 0; it < IT; ++it)
         if (RPI <= 16 || lane / CH < 16) *(Alias4*)(mine + it * RPI * LD) = res[it];
-      if (j + 1 < RJ) fetch(j + 1);
+      wave_exchange();
     }
-    wave_exchange();
+    i32x2_t o[FI];
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
-      Alias2* const at = (Alias2*)(lds + lr * LD + 32 * i + 8 * g);
       f32x4_t v = acc[i][j];
       if constexpr (AGPR) asm volatile("" : "+a"(v)::"memory");
       if constexpr (RES) {
-        const i32x2_t rv = *at;
+        const i32x2_t rv = *(const Alias2*)(lds + lr * LD + 32 * i + 8 * g);
         v[0] += bf16_lo((uint32_t)rv[0]);
         v[1] += bf16_hi((uint32_t)rv[0]);
         v[2] += bf16_lo((uint32_t)rv[1]);
         v[3] += bf16_hi((uint32_t)rv[1]);
       }
-      *at = i32x2_t{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3])};
+      o[i] = i32x2_t{(int)pack_bf16x2(v[0], v[1]), (int)pack_bf16x2(v[2], v[3])};
+    }
+    if (j > 0) {
+      store(j - 1);
+      wave_exchange();
+    }
+#pragma unroll
+    for (int i = 0; i < FI; ++i) *(Alias2*)(lds + lr * LD + 32 * i + 8 * g) = o[i];
+    if (j + 1 < RJ) {
+      rows(j + 1);
+      if constexpr (RES) fetch(j + 1);
     }
     wave_exchange();
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      const int64_t y = row_of(j, it);
-      if (y >= 0) *(i32x4_t*)(a.y[part] + y * ld + col) = *(const Alias4*)(mine + it * RPI * LD);
-    }
+    for (int it = 0; it < IT; ++it) q[it] = *(const Alias4*)(mine + it * RPI * LD);
     wave_exchange();
   }
+  store(RJ - 1);
 }
 // (One branch: a load that some path leaves in flight would have the compiler wait for all transfers in the next loop.)
 template <bool AGPR, int FI, int RJ>
-__device__ __forceinline__ void put_tile(const F8GemmK& a, const int64_t* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
+__device__ __forceinline__ void put_tile(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
   if (a.res) put_rows<AGPR, true>(a, yrow, nw, acc, lds, lane);
   else put_rows<AGPR, false>(a, yrow, nw, acc, lds, lane);
 }
@@ -311,7 +328,7 @@ __device__ __forceinline__ int chunk_swz(int c, int row) { return c ^ ((row >> 1
 __host__ __device__ constexpr int tile_x_scales(int bm, int ld) { return (bm * ld + 255) / 256 * 256; }
 __host__ __device__ constexpr int tile_w_scales(int bn, int ld) { return (bn + kF8Group - 1) / kF8Group * ((ld + 255) / 256 * 256); }
 __host__ __device__ constexpr int tile_fixed(int bn, int bm, int nst, int ld, int run) {
-  return nst * (bn + bm) * kF8Group + tile_x_scales(bm, ld) + run * tile_w_scales(bn, ld) + 8 * bm;
+  return nst * (bn + bm) * kF8Group + tile_x_scales(bm, ld) + run * tile_w_scales(bn, ld) + 4 * bm;
 }
 
 // A block of k of a run: its tile, the block, its stage, and for its transfers: the stage's address in LDS with the wave's
@@ -340,7 +357,7 @@ struct Feed {
   uint32_t woff[PW];
   const uint8_t* src[PX];
   uint32_t lds0, xs_at, ws_at;
-  int64_t* yrow;               // of the wave's rows
+  int* yrow;                   // of the wave's rows
   char* out;                   // the wave's place for results
 
   __device__ __forceinline__ Feed(const F8GemmK& arg, int tid)
@@ -424,10 +441,10 @@ struct Feed {
     const uint32_t xs0 = lds0 + NST * STAGE, ws0 = xs0 + tile_x_scales(BM, a.ld);
     xs_at = xs0 + 4 * (wm * (BM / WM) + lr);
     ws_at = ws0 + (n0 % kF8Group + wn * (BN / WN)) / kF8Group * ((a.ld + 255) / 256 * 256);
-    int64_t* const rows = (int64_t*)(smem + tile_fixed(BN, BM, NST, a.ld, a.run) - 8 * BM);
+    int* const rows = (int*)(smem + tile_fixed(BN, BM, NST, a.ld, a.run) - 4 * BM);
     yrow = rows + wm * (BM / WM);
     out = (a.run > 1 ? smem + tile_fixed(BN, BM, NST, a.ld, a.run) : smem) + wu * epilogue_lds<FI>();
-    if (lane + 64 * wu < BM) rows[lane + 64 * wu] = t.m0 + lane + 64 * wu < t.nr ? y_row<EXPERTS>(a, t, t.m0 + lane + 64 * wu) : -1;
+    if (lane + 64 * wu < BM) rows[lane + 64 * wu] = t.m0 + lane + 64 * wu < t.nr ? (int)y_row<EXPERTS>(a, t, t.m0 + lane + 64 * wu) : -1;
     if constexpr (BM > 64 * NW) static_assert(BM <= 64 * NW, "a row a thread");
     SX_WAIT_VM(0);   // the indices above are the compiler's loads
     for (int q = wu; q < tile_x_scales(BM, a.ld) / 256; q += NW) {
