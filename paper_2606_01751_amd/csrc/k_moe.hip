@@ -79,6 +79,10 @@ __device__ __forceinline__ float share(float v, float m) { return v == m ? 1.0f 
 // counts are there, a second pass places the rows, 64 at a time: no row takes an expert twice, so 64 bits an expert say
 // which rows take it, and the number of bits below a row's own is its rank.  With one workgroup both passes are one
 // launch.
+//
+// Bound by latency: 64 rows x 128 experts of float32 6.5 us, of which top_k rounds of a maximum over 16 lanes are most;
+// 32767 rows of bfloat16 8.2 + 7.8 us (11.5 MB), 256 workgroups, each of which sums all workgroups' counts.  64 rows a
+// workgroup where 256 of them are enough: 4096 rows x 256 of float32 14 us, 33 with 256 rows a workgroup.
 // ---------------------------------------------------------------------------------------------
 struct RouteLds {
   int base[kMoeMaxExperts];              // counts, later the next place of every expert
