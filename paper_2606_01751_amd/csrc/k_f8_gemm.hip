@@ -115,23 +115,6 @@ __device__ __forceinline__ int64_t y_row(const F8GemmK& a, const RowTile& t, int
   }
 }
 
-// Four consecutive features n of a row of y.
-__device__ __forceinline__ void put4(const F8GemmK& a, int64_t row, int part, int n, f32x4_t v) {
-  if (row < 0) return;
-  const int64_t at = row * (a.pn[part + 1] - a.pn[part]) + (n - a.pn[part]);
-  if (a.res) {
-    const uint2 rv = *(const uint2*)(a.res + at);
-    v[0] += bf16_lo(rv.x);
-    v[1] += bf16_hi(rv.x);
-    v[2] += bf16_lo(rv.y);
-    v[3] += bf16_hi(rv.y);
-  }
-  uint2 o;
-  o.x = pack_bf16x2(v[0], v[1]);
-  o.y = pack_bf16x2(v[2], v[3]);
-  *(uint2*)(a.y[part] + at) = o;
-}
-
 __device__ __forceinline__ int part_of(const F8GemmK& a, int n) {
   int p = 0;
   while (p + 1 < a.n_parts && n >= a.pn[p + 1]) ++p;
@@ -153,9 +136,13 @@ __device__ __forceinline__ void wave_exchange() {
 template <int FI>
 constexpr int epilogue_lds() { return 16 * (32 * FI + 16); }   // (16 bytes a row against bank conflicts)
 // AGPR: the sums are in accumulation registers; the empty asm keeps the compiler from fetching all of them at once.
-template <bool AGPR, bool RES, int FI, int RJ>
-__device__ __forceinline__ void put_rows(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
-  constexpr int LD = 32 * FI + 16, CH = 2 * FI, RPI = 64 / CH, IT = (16 + RPI - 1) / RPI;   // 16-byte chunks of a row, rows an instruction
+// PRE: `pre` holds the residual already, of all rows.
+template <int FI>
+constexpr int put_loads() { return (16 + 32 / FI - 1) / (32 / FI); }   // instructions for 16 rows
+template <bool AGPR, bool RES, bool PRE, int FI, int RJ>
+__device__ __forceinline__ void put_rows(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ],
+                                         const i32x4_t (&pre)[RJ][put_loads<FI>()], char* lds, int lane) {
+  constexpr int LD = 32 * FI + 16, CH = 2 * FI, RPI = 64 / CH, IT = put_loads<FI>();   // 16-byte chunks of a row, rows an instruction
   static_assert(64 % CH == 0, "whole rows an instruction");
   const int lr = lane % 16, g = lane / 16;
   const int part = part_of(a, nw);
@@ -172,7 +159,10 @@ __device__ __forceinline__ void put_rows(const F8GemmK& a, const int* yrow, int 
   };
   auto fetch = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-    for (int it = 0; it < IT; ++it) res[it] = row[j % 2][it] >= 0 ? *(const i32x4_t*)(from + (uint64_t)(uint32_t)row[j % 2][it] * ld) : i32x4_t{};
+    for (int it = 0; it < IT; ++it) {
+      if constexpr (PRE) res[it] = pre[j][it];
+      else res[it] = row[j % 2][it] >= 0 ? *(const i32x4_t*)(from + (uint64_t)(uint32_t)row[j % 2][it] * ld) : i32x4_t{};
+    }
   };
   char* const mine = lds + lane / CH * LD + lane % CH * 16;
   auto store = [&](int j) __attribute__((always_inline)) {
@@ -222,10 +212,16 @@ __device__ __forceinline__ void put_rows(const F8GemmK& a, const int* yrow, int 
   store(RJ - 1);
 }
 // (One branch: a load that some path leaves in flight would have the compiler wait for all transfers in the next loop.)
+template <bool AGPR, bool PRE, int FI, int RJ>
+__device__ __forceinline__ void put_tile(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ],
+                                         const i32x4_t (&pre)[RJ][put_loads<FI>()], char* lds, int lane) {
+  if (a.res) put_rows<AGPR, true, PRE>(a, yrow, nw, acc, pre, lds, lane);
+  else put_rows<AGPR, false, PRE>(a, yrow, nw, acc, pre, lds, lane);
+}
 template <bool AGPR, int FI, int RJ>
 __device__ __forceinline__ void put_tile(const F8GemmK& a, const int* yrow, int nw, const f32x4_t (&acc)[FI][RJ], char* lds, int lane) {
-  if (a.res) put_rows<AGPR, true>(a, yrow, nw, acc, lds, lane);
-  else put_rows<AGPR, false>(a, yrow, nw, acc, lds, lane);
+  const i32x4_t none[RJ][put_loads<FI>()] = {};
+  put_tile<AGPR, false>(a, yrow, nw, acc, none, lds, lane);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -254,6 +250,18 @@ __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
     const int64_t row = x_row<EXPERTS>(a, t, min(t.m0 + 16 * j + lr, t.nr - 1));
     x[j] = a.x + row * a.K + 16 * g;
     xs[j] = a.xs + row * a.ld;
+  }
+  // four consecutive features of a row a lane and fragment: where they go, and the residual ahead of all else
+  const int part = part_of(a, n0), ld = a.pn[part + 1] - a.pn[part], col = n0 - a.pn[part] + 4 * g;
+  int64_t y[RJ];
+  uint2 res[FI][RJ];
+#pragma unroll
+  for (int j = 0; j < RJ; ++j) {
+    const int m = t.m0 + 16 * j + lr;
+    y[j] = m < t.nr ? y_row<EXPERTS>(a, t, m) : -1;
+    if (!EXPERTS && a.res)
+#pragma unroll
+      for (int i = 0; i < FI; ++i) res[i][j] = y[j] >= 0 ? *(const uint2*)(a.res + y[j] * ld + col + 16 * i) : make_uint2(0, 0);
   }
   f32x4_t acc[FI][RJ];
 #pragma unroll
@@ -299,14 +307,20 @@ __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
   };
   for (int b = 0; b < nb; b += D)
     [&]<int... S>(std::integer_sequence<int, S...>) { (step(std::integral_constant<int, S>{}, b), ...); }(std::make_integer_sequence<int, D>{});
-  const int part = part_of(a, n0);
 #pragma unroll
   for (int j = 0; j < RJ; ++j) {
-    const int m = t.m0 + 16 * j + lr;
-    if (m < t.nr) {
-      const int64_t row = y_row<EXPERTS>(a, t, m);
+    if (y[j] >= 0) {
 #pragma unroll
-      for (int i = 0; i < FI; ++i) put4(a, row, part, n0 + 16 * i + 4 * g, acc[i][j]);
+      for (int i = 0; i < FI; ++i) {
+        f32x4_t v = acc[i][j];
+        if (!EXPERTS && a.res) {
+          v[0] += bf16_lo(res[i][j].x);
+          v[1] += bf16_hi(res[i][j].x);
+          v[2] += bf16_lo(res[i][j].y);
+          v[3] += bf16_hi(res[i][j].y);
+        }
+        *(uint2*)(a.y[part] + y[j] * ld + col + 16 * i) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      }
     }
   }
 }
@@ -412,7 +426,7 @@ struct Feed {
   // The workgroup's run, its addresses and its scale bytes on their way; false where there is nothing to do.
   // Tile order: groups of kRowGroup row tiles, the run slowest within a group; block b runs on XCD b mod 8, and each XCD
   // takes a contiguous part of the order, so its workgroups read the same slices of w and x through one L2.
-  __device__ __forceinline__ bool start(char* smem, Place* fill) {
+  __device__ __forceinline__ bool start(char* smem, Place* fill, i32x4_t (*pre)[put_loads<FI>()] = nullptr) {
     const int n_nt = (a.N + BN - 1) / BN, n_runs = (n_nt + a.run - 1) / a.run;
     const unsigned per_xcd = gridDim.x / kXcds;   // the grid is a multiple of kXcds
     const unsigned L = blockIdx.x % kXcds * per_xcd + blockIdx.x / kXcds;
@@ -455,7 +469,20 @@ struct Feed {
     out = (a.run > 1 ? smem + tile_fixed(BN, BM, NST, a.ld, a.run) : smem) + wu * epilogue_lds<FI>();
     if (lane + 64 * wu < BM) rows[lane + 64 * wu] = t.m0 + lane + 64 * wu < t.nr ? (int)y_row<EXPERTS>(a, t, t.m0 + lane + 64 * wu) : -1;
     if constexpr (BM > 64 * NW) static_assert(BM <= 64 * NW, "a row a thread");
-    SX_WAIT_VM(0);   // the indices above are the compiler's loads
+    if (!EXPERTS && pre && a.res) {   // the residual, ahead of all transfers (of one tile, whose sums it meets in put_rows)
+      constexpr int CH = 2 * FI, RPI = 64 / CH;
+      const int col = n0 + wn * (BN / WN) + lane % CH * 8;
+#pragma unroll
+      for (int j = 0; j < RJ; ++j)
+#pragma unroll
+        for (int it = 0; it < put_loads<FI>(); ++it) {
+          const int m = t.m0 + wm * (BM / WM) + 16 * j + it * RPI + lane / CH;
+          const int64_t y = (RPI > 16 && lane / CH >= 16) || m >= t.nr ? -1 : y_row<EXPERTS>(a, t, m);
+          pre[j][it] = y >= 0 ? *(const i32x4_t*)(a.res + y * a.N + col) : i32x4_t{};
+        }
+    } else {
+      SX_WAIT_VM(0);   // the indices above are the compiler's loads
+    }
     for (int q = wu; q < tile_x_scales(BM, a.ld) / 256; q += NW) {
       const int i = min(q * 64 + lane, BM * words - 1);
       dma_word(a.xs + x_row<EXPERTS>(a, t, min(t.m0 + i % BM, t.nr - 1)) * a.ld + 4 * (i / BM), xs0 + q * 256);
@@ -684,7 +711,8 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   F f(a, threadIdx.x);
   Place fill;
-  if (!f.start(smem, &fill)) return;
+  i32x4_t pre[RJ][put_loads<FI>()] = {};
+  if (!f.start(smem, &fill, pre)) return;
 #pragma unroll
   for (int b = 0; b < NST; ++b) {
 #pragma unroll
@@ -748,7 +776,7 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_narrow_kernel(F8GemmK a) {
   const int nw = f.n0 + f.wn * (BN / WN);
   __builtin_amdgcn_s_waitcnt(0xF | (3 << 14) | (0x7 << 4));
   __syncthreads();   // (all waves have read the stages)
-  if (nw < a.N) put_tile<false>(a, f.yrow, nw, acc, f.out, f.lane);
+  if (nw < a.N) put_tile<false, true>(a, f.yrow, nw, acc, pre, f.out, f.lane);
 }
 
 // Row tiles of BM rows that the launch may have to take.
