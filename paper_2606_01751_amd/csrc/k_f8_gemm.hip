@@ -861,8 +861,8 @@ constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for gr
 // (13.9, 14.2), 200 x 4096 13.2 (16.3, 18.1), 394 x 4096 18.5 (19.7, 22.2), 1000 x 4096 25.2 (28.8, 37.2), 2048 x 4096 43 (48, 60),
 // 6712 x 28672 669 (881).
 // Grouped rows: few for each expert, by the streaming kernel, since the weights' way from memory is the bound (64 tokens x 8
-// of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, 2048 -> 3072: 185, 166); else by the same costs and as
-// many tiles as rows spread over the experts make, each expert's last one half full (2048 -> 3072: 512 x 8 of 128 193 us of
+// of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, twice as wide: 185, 166); else by the same costs and as
+// many tiles as rows spread over the experts make, each expert's last one half full (2048 -> 2 x 1536: 512 x 8 of 128 193 us of
 // 128 x 64, 213 of 128 x 128; 2048 x 2 of 8 42 of 128 x 128, 48 of 128 x 64, 60 of 256 x 256; 8192 x 8 of 128 574 of 256 x 256, 688 of
 // 128 x 128; of 26 such products within 7% of the fastest but for five, which are 9 to 20% off).
 int best_shape(const F8GemmK& a, int n_cu) {
