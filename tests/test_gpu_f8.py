@@ -319,7 +319,7 @@ def codes(g, rows, k, n=None):
 LARGE = [(16, 6144, 4096), (40, 4096, 4096), (64, 4224, 4096), (180, 4224, 4096), (394, 4224, 4096), (1000, 3968, 4096),
          (2048, 4096, 4096), (2500, 11136, 2048), (8100, 8064, 512), (4100, 4992, 128), (6400, 4992, 128), (1450, 8320, 128),
          (4900, 6528, 896), (700, 12160, 1152), (20, 4224, 16512), (40, 4224, 16512), (200, 2048, 33280), (600, 2048, 16512),
-         (1100, 2048, 16512), (200, 8320, 128), (40, 8320, 512), (2000, 8320, 128)]
+         (1100, 2048, 16512), (200, 8320, 128), (40, 8320, 512), (2000, 8320, 128), (4100, 4224, 15360)]
 
 
 @pytest.mark.parametrize("rows,n,k", LARGE)
