@@ -227,7 +227,7 @@ __device__ __forceinline__ void put_tile(const F8GemmK& a, const int* yrow, int 
 // ---------------------------------------------------------------------------------------------
 // Few rows: a wave of its own takes 16 FI features and 16 RJ rows and reads both operands from memory into registers, D
 // blocks of k ahead, so no wave waits for another and nothing passes through LDS.  Bound by memory where every weight serves
-// one wave (64 tokens x 8 of 128 experts, 2048 -> 1536: 322 MB in 60 us, 5.4 TB/s; 1 row x 4096 x 14336, 59 MB in 21 us), and
+// one wave (64 tokens x 8 of 128 experts, 2048 -> 1536: 322 MB in 60 us, 5.4 TB/s; 1 row x 4096 x 14336, 59 MB in 17 us), and
 // beyond by the loads, whose instructions touch 16 lines of memory for a kilobyte (64 rows x 6144 x 4096: 26 us, 12 by 64 x 32
 // tiles through LDS).
 // ---------------------------------------------------------------------------------------------
@@ -849,7 +849,7 @@ struct Shape {
 };
 enum { kStream, k32x32, k64x32, k64x64, k128x64, k128x128, k128x128x2, k256x256, kShapes };
 constexpr Shape kShape[kShapes] = {
-    {16, 16, 0, 64, 1, 2.70, 0.155, 0.03, 0.113},    {32, 32, 6, 256, 1, 3.68, 0.193, 0.84, 0.093},
+    {16, 16, 0, 64, 1, 2.99, 0.134, 0.01, 0.115},    {32, 32, 6, 256, 1, 3.68, 0.193, 0.84, 0.093},
     {64, 32, 6, 256, 1, 3.71, 0.220, 1.26, 0.148},   {64, 64, 4, 256, 1, 3.62, 0.294, 1.45, 0.200},
     {128, 64, 3, 512, 1, 3.19, 0.474, 2.09, 0.310},  {128, 128, 4, 512, 1, 4.42, 0.554, 4.38, 0.591},
     {128, 128, 2, 512, 2, 3.00, 1.040, 9.23, 0.973}, {256, 256, 2, 256, 1, 7.90, 1.414, 10.69, 1.437}};
@@ -857,9 +857,9 @@ constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 4096;   // of a launch (and
 constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for grouped rows (of listed ones: 16)
 
 // The shape of least time; for those 105 products within 4% of the fastest (0.1% in the mean).  Some of them in us, the shape
-// taken and its neighbours in the table: K = 4096, 1 row x 4096 features 8.8 (9.9), 17 x 6144 10.2 (13.7, 10.9), 64 x 6144 11.8
-// (13.9, 14.2), 200 x 4096 13.2 (16.3, 18.1), 394 x 4096 18.5 (19.7, 22.2), 1000 x 4096 25.2 (28.8, 37.2), 2048 x 4096 43 (48, 60),
-// 6712 x 28672 669 (881).
+// taken and its neighbours in the table: K = 4096, 1 row x 4096 features 7.9 (9.9), 1 x 6144 9.5 (10.8), 17 x 6144 10.2 (13.9,
+// 10.9), 64 x 6144 11.8 (13.9, 14.2), 200 x 4096 13.2 (16.3, 18.1), 394 x 4096 18.5 (19.7, 22.2), 1000 x 4096 25.2 (28.8, 37.2),
+// 2048 x 4096 43 (48, 60), 6712 x 28672 669 (881).
 // Grouped rows: few for each expert, by the streaming kernel, since the weights' way from memory is the bound (64 tokens x 8
 // of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, twice as wide: 185, 166); else by the same costs and as
 // many tiles as rows spread over the experts make, each expert's last one half full (2048 -> 2 x 1536: 512 x 8 of 128 193 us of
@@ -883,7 +883,9 @@ int best_shape(const F8GemmK& a, int n_cu) {
       tiles = a.n_experts * (full > 0.5 ? full + 0.5 : 1) * (double)n_tiles + n_cu / 8;
     }
     const double rounds = ceil(tiles / ((double)n_cu * h.occ));
-    const double t = h.first + nb * h.block + (rounds - 1) * (h.more + nb * h.more_block);
+    // (a streaming wave's loads touch 16 lines of w and one of x for each of up to 16 rows)
+    const double lines = i == kStream && a.r.max_rows < 16 ? (16 + a.r.max_rows) / 32.0 : 1.0;
+    const double t = h.first + nb * h.block + (rounds - 1) * (h.more + nb * h.more_block * lines);
     if (t < least) {
       least = t;
       best = i;
@@ -896,7 +898,12 @@ int best_shape(const F8GemmK& a, int n_cu) {
 
 hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
   switch (best_shape(a, n_cu)) {
-    case kStream: return a.offsets ? launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4>(a, s) : launch_stream<1, 1, 8>(a, s);
+    case kStream:
+      if (a.offsets) return launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4>(a, s);
+      // Blocks ahead: 16 of them leave room for one wave a SIMD, which then has more on its way (1 row x 4096 x 14336 17.0 us,
+      // 18.3 with 12, 20.3 with 8); where there are more waves, or few blocks, 12 (1 x 28672 x 4096 27.7, 29.6 with 16).
+      if (a.K >= 16 * kF8Group && count_tiles(a, 16) * (a.N / 16) <= 4 * (int64_t)n_cu) return launch_stream<1, 1, 16>(a, s);
+      return launch_stream<1, 1, 12>(a, s);
     case k32x32: return launch_narrow<32, 32, 2, 2, 6>(a, n_cu, s);
     case k64x32: return launch_narrow<64, 32, 2, 2, 6>(a, n_cu, s);
     case k64x64: return launch_narrow<64, 64, 2, 2, 4>(a, n_cu, s);
