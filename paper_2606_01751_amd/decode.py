@@ -26,6 +26,8 @@ _TYPES = {F32: torch.float32, BF16: torch.bfloat16}
 _I32, _U8 = torch.int32, torch.uint8
 # the current stream's handle on a GPU without a Stream object (2.5 us), where torch offers it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# torch.cuda.current_device without its look whether the GPU is in use yet, which a tensor there answers
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _need(ok: bool, what: str):
@@ -44,7 +46,7 @@ def _int(v, what: str) -> int:
 def _device(t) -> int:
     """The GPU that a call's tensors have to be on: the current one, where its first tensor is."""
     at = t.get_device()      # -1: host memory
-    if at < 0 or at != torch.cuda.current_device():
+    if at < 0 or at != _current():
         raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
     return at
 

@@ -82,6 +82,8 @@ def _entries(t, n: int, at: int, what: str):
     """Pointer of an int32 array of at least n entries."""
     if not isinstance(t, torch.Tensor) or t.numel() < n:
         raise ValueError(f"{what} must be an int32 tensor of {n} entries")
+    if t.dtype is _I32 and t.get_device() == at and t.is_contiguous():
+        return t.data_ptr()
     return _ptr(t, _I32, at, what)
 
 
@@ -93,9 +95,11 @@ def _index(t, n: int, at: int, what: str):
 def _row_args(plan, rows, n_rows, max_rows, have: int, at: int):
     """(plan handle, rows, n_rows, max_rows) of a call whose arrays have `have` rows."""
     if plan is None:
-        _need(rows is None, "a row list needs a plan")
-        n = _int(have if max_rows is None else max_rows, "max_rows")
-        _need(n <= have, f"max_rows {n} exceeds the arrays' {have} rows")
+        if rows is not None:
+            raise ValueError("a row list needs a plan")
+        n = have if max_rows is None else max_rows
+        if not -0x80000000 <= n <= have or n > 0x7fffffff:   # (a negative one is the library's to refuse)
+            raise ValueError(f"max_rows {n} exceeds the arrays' {have} rows or 32 bits")
         return None, None, None if n_rows is None else _entries(n_rows, 1, at, "n_rows"), n
     info = plan.info()
     total = info["total_tokens"]
@@ -133,7 +137,8 @@ def add_rmsnorm_f8(x, y8, y_scale, gamma=None, eps: float = 1e-6, delta=None, x_
         yp = sp = None
     else:
         yp, sp = _matrix(y8, _CODES, have, h, at, "y8"), _matrix(y_scale, _SCALES, have, _ld(h), at, "y_scale")
-    _need(gamma is None or gamma.numel() == h, f"gamma must have {h} elements")
+    if gamma is not None and gamma.numel() != h:
+        raise ValueError(f"gamma must have {h} elements")
     p, rp, np_, m = _row_args(plan, rows, n_rows, max_rows, have, at)
     _check(lib().sx_add_rmsnorm_f8(
         p, rp, np_, m, xp, 1 if x_by_token else 0, _like(delta, have, h, at, "delta"), _opt(gamma, _BF16, at, "gamma"), eps, h,
@@ -185,14 +190,17 @@ def moe_route(logits, ids, weights, offsets, order, workspace, renormalise=True,
     """ids, weights [..][top_k] of the rows' top experts by logits [..][experts] (float32 or bfloat16), and their places
     grouped by expert: offsets [experts + 1], order [rows * top_k]."""
     at, have = _device(logits), logits.shape[0]
-    _need(logits.dim() == 2 and ids.dim() == 2, "logits must be [rows][experts] and ids [rows][top_k]")
-    _need(logits.dtype in (_F32, _BF16), f"logits must be float32 or bfloat16, not {logits.dtype}")
-    e, top = logits.shape[1], ids.shape[1]
-    _need(offsets.numel() == e + 1 and order.numel() == have * top, "offsets needs experts + 1 and order rows * top_k entries")
+    if logits.dim() != 2 or ids.dim() != 2:
+        raise ValueError("logits must be [rows][experts] and ids [rows][top_k]")
+    dtype, e, top = logits.dtype, logits.shape[1], ids.shape[1]
+    if dtype is not _F32 and dtype is not _BF16:
+        raise ValueError(f"logits must be float32 or bfloat16, not {dtype}")
+    if offsets.numel() != e + 1 or order.numel() != have * top:
+        raise ValueError("offsets needs experts + 1 and order rows * top_k entries")
     p, _, np_, m = _row_args(plan, None, n_rows, max_rows, have, at)
     _check(lib().sx_moe_route(
-        p, np_, m, _ptr(logits, logits.dtype, at, "logits"), F32 if logits.dtype is _F32 else BF16, e, top,
-        int(bool(renormalise)), _matrix(ids, (_I32,), have, top, at, "ids"), _matrix(weights, (_F32,), have, top, at, "weights"),
+        p, np_, m, _ptr(logits, dtype, at, "logits"), F32 if dtype is _F32 else BF16, e, top,
+        1 if renormalise else 0, _matrix(ids, (_I32,), have, top, at, "ids"), _matrix(weights, (_F32,), have, top, at, "weights"),
         _ptr(offsets, _I32, at, "offsets"), _ptr(order, _I32, at, "order"), _ptr(workspace, torch.uint8, at, "workspace"),
         workspace.numel(), _on(stream, at)))
 
@@ -208,9 +216,9 @@ def gemm_experts_f8(x8, x_scale, w8, w_scale, offsets, order, y, gather: int = 0
     e = w8.shape[0]
     _need(offsets.numel() == e + 1, "offsets needs experts + 1 entries")
     _check(lib().sx_gemm_experts_f8(
-        _ptr(offsets, _I32, at, "offsets"), None if order is None else _entries(order, places, at, "order"), e, _int(places, "places"), xp, xsp,
-        _int(x_rows, "rows of x"), _int(gather, "gather"), _matrix(w8, _CODES, e * n, k, at, "w8"),
-        _matrix(w_scale, _SCALES, e * (n // 128), _ld(k), at, "w_scale"), k, n, yp, int(bool(scatter)), _on(stream, at)))
+        _ptr(offsets, _I32, at, "offsets"), None if order is None else _entries(order, places, at, "order"), e,
+        _int(places, "places"), xp, xsp, _int(x_rows, "rows of x"), _int(gather, "gather"), _matrix(w8, _CODES, e * n, k, at, "w8"),
+        _matrix(w_scale, _SCALES, e * (n // 128), _ld(k), at, "w_scale"), k, n, yp, 1 if scatter else 0, _on(stream, at)))
 
 
 def moe_combine(y, weights, out, residual=None, plan: Plan = None, rows=None, n_rows=None, max_rows=None,
@@ -221,7 +229,9 @@ def moe_combine(y, weights, out, residual=None, plan: Plan = None, rows=None, n_
     _need(weights.dim() == 2, "weights must be [rows][top_k]")
     top = weights.shape[1]
     yp, w = _wide(y, have * top, at, "y")
-    _need(w == h, f"y must be [{have * top}][{h}], not {list(y.shape)}")
+    if w != h:
+        raise ValueError(f"y must be [{have * top}][{h}], not {list(y.shape)}")
     p, rp, np_, m = _row_args(plan, rows, n_rows, max_rows, have, at)
-    _check(lib().sx_moe_combine(p, rp, np_, m, yp, _matrix(weights, (_F32,), have, top, at, "weights"), top, h,
-                                _like(residual, have, h, at, "residual"), op, int(bool(out_by_token)), _on(stream, at)))
+    _check(lib().sx_moe_combine(
+        p, rp, np_, m, yp, _matrix(weights, (_F32,), have, top, at, "weights"), top, h, _like(residual, have, h, at, "residual"), op,
+        1 if out_by_token else 0, _on(stream, at)))

@@ -209,6 +209,13 @@ def test_binding_takes_no_number_for_a_count_or_an_order():
     for bad in (5, 5.0, [5], torch.zeros(0, dtype=torch.int32)):
         with pytest.raises(ValueError, match="int32 tensor"):
             layer8._row_args(None, None, bad, None, 8, 0)
+    for bad in (9, 1 << 32, 5 - (1 << 32)):        # (which 32 bits would hold as 9, 0 and 5)
+        with pytest.raises(ValueError, match="exceeds"):
+            layer8._row_args(None, None, None, bad, 8, 0)
+    with pytest.raises(ValueError, match="exceeds"):
+        layer8._row_args(None, None, None, None, 1 << 31, 0)
+    with pytest.raises(ValueError, match="needs a plan"):
+        layer8._row_args(None, torch.zeros(8, dtype=torch.int32), None, 8, 8, 0)
 
 
 def test_e4m3_reference_against_torch():
