@@ -347,11 +347,13 @@ __global__ __launch_bounds__(512, 1) void attn_mfma_kernel(AttnK ka) {
       // the base is wave-uniform; readfirstlane makes that visible where the compiler cannot prove it
       // (the instruction takes its base from an SGPR pair)
       // (the builtin returns a signed int: each half goes through uint32_t so that nothing is sign-extended)
+      // A memory instruction may read a scalar register five wait states after a vector instruction, such as
+      // readfirstlane, wrote it; the compiler does not see into the statement, so they are kept here.
       const uint64_t sb = (uint64_t)(uintptr_t)sbase;
       const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)sb);
       const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(sb >> 32));
       const uint64_t sbu = ((uint64_t)hi << 32) | (uint64_t)lo;
-      asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffset), "s"(sbu), "s"(m0)
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffset), "s"(sbu), "s"(m0)
                    : "m0", "memory");
     };
     // per-lane byte offsets of the transfers inside a (block, head) run; tiles start at multiples
@@ -1126,15 +1128,15 @@ __global__ __launch_bounds__(512, 2 * WGS) void colsum_kernel(ColsumK a) {
     const uint32_t hi32 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(sb >> 32));
     return ((uint64_t)hi32 << 32) | (uint64_t)lo32;
   };
-  // (dst: LDS byte address, wave-uniform)
+  // (dst: LDS byte address, wave-uniform; five wait states between the readfirstlanes of the base and its use)
   auto dma16_sb = [&](uint64_t sbase, uint32_t voffset, uint32_t dst) {
     const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)dst);
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffset), "s"(sbase), "s"(m0)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffset), "s"(sbase), "s"(m0)
                  : "m0", "memory");
   };
   auto dma4_sb = [&](uint64_t sbase, uint32_t voffset, uint32_t dst) {
     const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)dst);
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" ::"v"(voffset), "s"(sbase), "s"(m0)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dword %0, %1" ::"v"(voffset), "s"(sbase), "s"(m0)
                  : "m0", "memory");
   };
   auto dma4 = [&](const void* src, uint32_t dst) {

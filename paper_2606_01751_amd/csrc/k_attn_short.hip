@@ -149,7 +149,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_short_kernel(AttnS a) {
 #pragma unroll
         for (int i = 0; i < NT / 2; ++i) {
           const uint32_t m0 = __builtin_amdgcn_readfirstlane(dst + (uint32_t)((b * NT / 2 + i) * 1024));
-          asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(is_v ? off_v[i] : off_k[i]), "s"(sbu),
+          // (five wait states between the readfirstlanes of the base and its use)
+          asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(is_v ? off_v[i] : off_k[i]), "s"(sbu),
                        "s"(m0)
                        : "m0", "memory");
         }

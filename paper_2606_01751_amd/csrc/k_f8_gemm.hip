@@ -402,15 +402,16 @@ struct Feed {
   }
 
   // Transfer d of this wave for the block at p; no lane takes part where there is none (a branch would let the compiler move
-  // matrix instructions over it).
+  // matrix instructions over it).  A memory instruction may read a scalar register five wait states after a vector
+  // instruction, such as readfirstlane, wrote it; the compiler does not see into the statement, so they are kept there.
   __device__ __forceinline__ void dma(const Place& p, int d) const {
     const int dw = __builtin_amdgcn_readfirstlane(p.dw), lanes = __builtin_amdgcn_readfirstlane(p.lanes);
     const uint32_t lds = __builtin_amdgcn_readfirstlane(p.lds);
     const uint64_t wp = (uint64_t)p.w;
     const uint64_t w = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(wp >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)wp);
     if (d < PW)
-      asm volatile("s_cmp_gt_i32 %2, %3\n\ts_cselect_b32 exec_lo, -1, 0\n\ts_cselect_b32 exec_hi, -1, 0\n\ts_add_u32 m0, %4, %5\n\t"
-                   "global_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(woff[d]), "s"(w), "s"(dw), "n"(d), "s"(lds),
+      asm volatile("s_add_u32 m0, %4, %5\n\ts_cmp_gt_i32 %2, %3\n\ts_cselect_b32 exec_lo, -1, 0\n\ts_cselect_b32 exec_hi, -1, 0\n\t"
+                   "s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(woff[d]), "s"(w), "s"(dw), "n"(d), "s"(lds),
                    "n"(NW * d * 1024)
                    : "m0", "scc", "memory");
     else
