@@ -337,10 +337,11 @@ __global__ __launch_bounds__(512, 1) void attn_mfma_kernel(AttnK ka) {
     // lands at dst + 16 l.  Issued as inline assembly so the compiler does not order every later
     // LDS read behind it: the wait for these transfers is explicit (vmcnt + barrier before a tile
     // is read).  The statement is volatile, so it stays between the barriers around it; it
-    // declares no memory clobber, which keeps the read-only index loads on the scalar unit.
+    // declares no memory clobber, which keeps the read-only index loads on the scalar unit.  M0 is
+    // written one wait state ahead of the transfer that reads it, which the compiler cannot see to.
     auto dma16 = [&](const void* src, const char* dst) {
       const uint32_t m0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)dst;
-      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(m0) : "m0", "memory");
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(m0) : "m0", "memory");
     };
     auto dma16_sb = [&](const uint16_t* sbase, uint32_t voffset, const char* dst) {
       const uint32_t m0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)dst;
@@ -1141,7 +1142,7 @@ __global__ __launch_bounds__(512, 2 * WGS) void colsum_kernel(ColsumK a) {
   };
   auto dma4 = [&](const void* src, uint32_t dst) {
     const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)dst);
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(m0) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(m0) : "m0", "memory");
   };
   const uint32_t smem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   auto issue = [&](int k) {

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_short_kernel(AttnS a) {
       const int ch = tch ^ (is_v ? v_swz<NCH>(row) : (row & (NCH - 1)));
       const uint16_t* p = base + bo[RPK * i / 16] + (min(key + row, last_key) - 16 * b) * rstride + ch * 8;
       const uint32_t m0 = __builtin_amdgcn_readfirstlane(dst + (uint32_t)(i * 1024));
-      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(m0) : "m0", "memory");
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(m0) : "m0", "memory");
     }
   };
 
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(SW * 64, 2) void lse_short_kernel(AttnS a) {
       const int row = RPK * i + trow;
       const uint16_t* p = a.k + bo[RPK * i / 16] + row_off(2 * t + RPK * i / 16, row & 15) + (tch ^ (row & (NCH - 1))) * 8;
       const uint32_t m0 = __builtin_amdgcn_readfirstlane(kb + (uint32_t)(i * 1024));
-      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(m0) : "m0", "memory");
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(m0) : "m0", "memory");
     }
   };
   uint32_t ko[NK];   // K operand: lane reads row l32, chunk 2 s + hg

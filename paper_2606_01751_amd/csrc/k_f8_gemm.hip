@@ -403,7 +403,8 @@ struct Feed {
 
   // Transfer d of this wave for the block at p; no lane takes part where there is none (a branch would let the compiler move
   // matrix instructions over it).  A memory instruction may read a scalar register five wait states after a vector
-  // instruction, such as readfirstlane, wrote it; the compiler does not see into the statement, so they are kept there.
+  // instruction, such as readfirstlane, wrote it, and a transfer to LDS m0 one wait
+  // state after a scalar instruction wrote it; the compiler does not see into the statement, so they are kept there.
   __device__ __forceinline__ void dma(const Place& p, int d) const {
     const int dw = __builtin_amdgcn_readfirstlane(p.dw), lanes = __builtin_amdgcn_readfirstlane(p.lanes);
     const uint32_t lds = __builtin_amdgcn_readfirstlane(p.lds);
@@ -415,13 +416,13 @@ struct Feed {
                    "n"(NW * d * 1024)
                    : "m0", "scc", "memory");
     else
-      asm volatile("s_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\ts_add_u32 m0, %2, %3\n\t"
+      asm volatile("s_add_u32 m0, %2, %3\n\ts_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\t"
                    "global_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1" ::"v"(src[d - PW] + p.b * kF8Group), "s"(lanes), "s"(lds),
                    "n"(BN * kF8Group + NW * (d - PW) * 1024)
                    : "m0", "scc", "memory");
   }
   __device__ __forceinline__ void dma_word(const uint8_t* from, uint32_t to) const {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
   }
 
   // The workgroup's run, its addresses and its scale bytes on their way; false where there is nothing to do.

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void gemm_rows_kernel(GemmRowsK a)
   auto dma = [&](int t, int d) {
     const uint32_t m0r = __builtin_amdgcn_readfirstlane(smem_lds + (uint32_t)((t % NST) * STAGE) +
                                                         (uint32_t)(d < PW ? (wu + NW * d) * 1024 : BN * ROWB + (wu + NW * (d - PW)) * 1024));
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src[d] + t * 64), "s"(m0r) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src[d] + t * 64), "s"(m0r) : "m0", "memory");
   };
   // wait until this wave's transfers of every stage before the n youngest have landed
   auto wait_stages = [&](int n) {

@@ -4,6 +4,7 @@ The gfx9 family leaves some waits between two instructions to whoever writes the
 instructions of its own; it cannot see into an asm statement, so what stands there, and what stands next to it, is checked
 here, in the disassembled kernels of libsx.so, along every path that leads to an instruction:
 
+  m0     a scalar instruction writes m0, a transfer to LDS reads it: 1
   base   a vector instruction writes a scalar register, a memory instruction reads it: 5
   dpp    a vector instruction writes a vector register, one that takes it from another lane (DPP) reads it: 2
   lane   a vector instruction writes a vector register, v_readlane or v_readfirstlane reads it: 1
@@ -59,6 +60,10 @@ def valu_writes(op, args):
     return out
 
 
+def m0_write(op, args):
+    return {("m0", 0)} if op.startswith("s_") and args and args[0] == "m0" and not op.startswith("s_cmp") else set()
+
+
 def scalar_of(op, args):
     return {r for r in valu_writes(op, args) if r[0] in ("s", "vcc")}
 
@@ -69,6 +74,7 @@ def vector_of(op, args):
 
 # name: (wait states, what is written by an instruction, what an instruction reads)
 RULES = {
+    "m0": (1, m0_write, lambda op, a: {("m0", 0)} if "_lds_" in op and is_memory(op) else set()),
     "base": (5, scalar_of, lambda op, a: {r for o in a for r in regs(o) if r[0] in ("s", "vcc")} if is_memory(op) else set()),
     "dpp": (2, vector_of, lambda op, a: {r for r in regs(a[1]) if r[0] == "v"} if op.endswith("_dpp") else set()),
     "lane": (1, vector_of, lambda op, a: {r for r in regs(a[1]) if r[0] == "v"} if op.startswith(("v_readlane", "v_readfirstlane")) else set()),
@@ -149,10 +155,12 @@ def listing(*lines):
 
 
 def test_the_check_finds_what_is_too_near():
-    # a base read after four wait states, after five, and around a loop
+    # a base read after four wait states, after five, and around a loop; m0 with and without a wait
     four = ["v_readfirstlane_b32 s4, v0", *["s_nop 0"] * 4, "global_load_lds_dwordx4 v1, s[4:5]"]
     assert missing(listing(*four), "base") == [("0x0", "0x14", 4)]
     assert missing(listing(four[0], "s_nop 4", four[-1]), "base") == []
+    assert missing(listing("s_mov_b32 m0, s1", four[-1]), "m0") == [("0x0", "0x4", 0)]
+    assert missing(listing("s_mov_b32 m0, s1", "s_nop 0", four[-1]), "m0") == []
     assert missing(listing("v_add_f32_e32 v1, v2, v3", "s_nop 0", "v_mov_b32_dpp v4, v1 row_ror:8 row_mask:0xf bank_mask:0xf"), "dpp") == [("0x0", "0x8", 1)]
     loop = "0000000000000000 <k>:\n\tglobal_load_dword v1, v2, s[4:5] // 000000000000: 0\n\tv_readlane_b32 s5, v0, 3 // 000000000004: 0\n" \
            "\ts_cbranch_scc1 65533 // 000000000008: 0 <k+0x0>\n\ts_endpgm // 00000000000C: 0\n"
