@@ -25,16 +25,15 @@ struct Arg {
   const char* name;
 };
 
-// Outputs `out` must not overlap each other or the inputs `in`, but where an output is listed in `same` as equal to an input.
+// Outputs `out` must not overlap each other or the inputs `in`; but out[0] may be in[in_place] itself (-1: none may).
 template <int NO, int NI>
-sx_status apart(const char* who, const Arg (&out)[NO], const Arg (&in)[NI], const void* may_out = nullptr,
-                const void* may_in = nullptr) {
+sx_status apart(const char* who, const Arg (&out)[NO], const Arg (&in)[NI], int in_place = -1) {
   for (int i = 0; i < NO; ++i) {
     for (int j = 0; j < i; ++j)
       if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
         return reportf(SX_EINVAL, "%s: %s and %s overlap", who, out[j].name, out[i].name);
     for (int j = 0; j < NI; ++j) {
-      if (may_in && out[i].p == may_out && in[j].p == may_in && out[i].p == in[j].p) continue;
+      if (i == 0 && j == in_place && out[i].p == in[j].p) continue;
       if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
         return reportf(SX_EINVAL, "%s: %s overlaps %s", who, out[i].name, in[j].name);
     }
@@ -146,7 +145,7 @@ sx_status sx_add_rmsnorm_f8(const sx_plan* plan, const int32_t* rows, const int3
                      {y_scale, total * sx::f8_ld(h), "y_scale"}};
   const Arg wide[] = {in[0], in[1], in[2]};
   if ((st = aligned(who, wide)) != SX_OK || (st = aligned(who, out)) != SX_OK) return st;
-  if ((st = apart(who, out, in, x_out, x)) != SX_OK) return st;
+  if ((st = apart(who, out, in, 0)) != SX_OK) return st;
   if (max_rows == 0) return SX_OK;
   a.x = (const uint16_t*)x;
   a.delta = (const uint16_t*)delta;
@@ -223,7 +222,7 @@ sx_status sx_gemm_f8(const sx_plan* plan, const int32_t* rows, const int32_t* n_
                     n_rows_arg(plan, n_rows)};
   const Arg wide[] = {in[0], in[1], in[2], in[3], in[4]};
   if ((st = aligned(who, wide)) != SX_OK || (st = aligned(who, out)) != SX_OK) return st;
-  if ((st = apart(who, out, in, y_parts[0], residual)) != SX_OK) return st;
+  if ((st = apart(who, out, in, 2)) != SX_OK) return st;
   if (max_rows == 0) return SX_OK;
   a.x = (const uint8_t*)x8;
   a.xs = (const uint8_t*)x_scale;
@@ -348,7 +347,7 @@ sx_status sx_moe_combine(const sx_plan* plan, const int32_t* rows, const int32_t
   const Arg to[] = {{out, total * 2 * h, "out"}};
   const Arg wide[] = {in[0], in[1], in[2]};
   if ((st = aligned(who, wide)) != SX_OK || (st = aligned(who, to)) != SX_OK) return st;
-  if ((st = apart(who, to, in, out, residual)) != SX_OK) return st;
+  if ((st = apart(who, to, in, 1)) != SX_OK) return st;
   if (max_rows == 0) return SX_OK;
   a.y = (const uint16_t*)y;
   a.weights = weights;

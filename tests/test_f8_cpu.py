@@ -157,6 +157,18 @@ def test_moe_combine_refusals(kw, want, text):
     err(combine(**kw), want, text)
 
 
+def test_an_output_may_be_one_input_and_no_other():
+    # x_out may be x, y the residual, out the residual: not what else lies at that address
+    err(norm(delta=at(1), xo=at(1)), V, "x_out overlaps delta")
+    err(norm(gamma=at(1), xo=at(1)), V, "x_out overlaps gamma")
+    err(norm(x=at(0), xo=at(0)), V, "x_out overlaps n_rows")
+    err(gemm(parts=1, x=at(5), res=at(5)), V, "y overlaps x8")
+    err(gemm(parts=1, w=at(5), res=at(5)), V, "y overlaps w8")
+    err(gemm(parts=1, ws=at(5), res=at(5)), V, "y overlaps w_scale")
+    err(combine(y=at(3), out=at(3)), V, "out overlaps y")
+    err(combine(wt=at(3), out=at(3)), V, "out overlaps weights")
+
+
 def test_nothing_to_do_is_fine():
     ok = sx.SX_OK
     assert norm(m=0) == ok and gemm(m=0) == ok and silu(m=0) == ok and combine(m=0) == ok and experts(places=0, off=None) == ok
