@@ -304,7 +304,8 @@ sx_status sx_gemm_experts_f8(const int32_t* offsets, const int32_t* order, int32
   if ((st = apart(who, out, in)) != SX_OK) return st;
   if (SX_DEVICE_CHECKS) {
     int v[4] = {0, 0, 0, 0};
-    hipError_t e = sx::device_check_offsets(offsets, n_experts, n_places, (hipStream_t)stream, v);
+    // (without gather a place is a row of x too)
+    hipError_t e = sx::device_check_offsets(offsets, n_experts, gather || x_rows > n_places ? n_places : x_rows, (hipStream_t)stream, v);
     if ((st = verdict(who, e, v)) != SX_OK) return st;
     if (order) {   // the places that are in use
       e = sx::device_check_order(offsets, n_experts, order, n_places, gather, gather ? x_rows : n_places, (hipStream_t)stream, v);

@@ -186,6 +186,30 @@ def test_gemm_experts_f8_places_not_in_use_and_bad_entries():
         sx.use_checked(False)
 
 
+@pytest.mark.parametrize("scatter", [False, True])
+def test_places_behind_the_rows_of_x(scatter):
+    # without gather a place is a row of x itself: the release library leaves those out that x does not have, the checked one refuses
+    g = gen(33)
+    n, k, sizes, have = 128, 256, [10, 0, 25, 7], 30
+    off = torch.tensor([0, 10, 10, 35, 42], dtype=torch.int32)
+    order = torch.randperm(50, generator=g).int() if scatter else None
+    wc, ws = expert_weights(g, len(sizes), n, k)
+    xc, xs = operands(g, 42, 128, k)[:2]
+    want = run_experts(xc, xs, wc, ws, off, order, 50, scatter=scatter)
+    short = run_experts(xc[:have], xs[:have], wc, ws, off, order, 50, scatter=scatter)
+    out = order[have:42].long() if scatter else torch.arange(have, 42)
+    want[out] = 7
+    assert torch.equal(short, want)
+    sx.use_checked(True)
+    try:
+        run_experts(xc, xs, wc, ws, off, order, 50, scatter=scatter)
+        with pytest.raises(sx.SxError) as err:
+            run_experts(xc[:have], xs[:have], wc, ws, off, order, 50, scatter=scatter)
+        assert err.value.status == sx.SX_EDEVICE
+    finally:
+        sx.use_checked(False)
+
+
 def test_an_experts_rows_are_those_of_the_plain_product():
     # the same bits as gemm_f8 with that expert's weight, however many rows the others have
     g = gen(32)
