@@ -41,7 +41,8 @@
  * the layer body in include/sx.h; listed rows beyond their request are left out.  plan == NULL: `rows` must
  * be NULL, the rows are 0 .. max_rows - 1 of every array, or the first min(*n_rows, max_rows) of them where
  * n_rows (DEVICE [1]) is given, as in a padded batch; the by_token arguments say nothing then.  Rows not
- * listed, and rows behind the last one, are neither read nor written.
+ * listed, and rows behind the last one, are neither read nor written.  A call may have no rows at all: its arrays of rows
+ * may then be NULL.
  *
  * Results: a call gives the same bits every time, and a row's results do not depend on the other rows of
  * the call, nor on how loose max_rows is: every product sums an element over k in one order, whatever tile

@@ -61,7 +61,7 @@ sx_status verdict(const char* who, hipError_t e, const int v[4]) {
   return SX_OK;
 }
 
-// The rows of a call; `total` is the number of rows of its arrays.
+// The rows of a call; `total` is the number of rows of its arrays, which may be NULL where there are none.
 sx_status rows_of(const char* who, const sx_plan* p, const int32_t* rows, const int32_t* n_rows, int32_t max_rows,
                   bool by_token, void* stream, sx::F8Rows* r, int64_t* total) {
   if (max_rows < 0) return reportf(SX_EINVAL, "%s: max_rows must be >= 0", who);
@@ -132,9 +132,9 @@ sx_status sx_add_rmsnorm_f8(const sx_plan* plan, const int32_t* rows, const int3
   sx_status st = rows_of(who, plan, rows, n_rows, max_rows, x_by_token || y_by_token, stream, &a.r, &total);
   if (st != SX_OK) return st;
   if ((st = width_ok(who, "h", h, 1 << 24)) != SX_OK) return st;
-  if (!x) return reportf(SX_EINVAL, "%s: x is NULL", who);
+  if (!x && total > 0) return reportf(SX_EINVAL, "%s: x is NULL", who);
   if (!y8 != !y_scale) return reportf(SX_EINVAL, "%s: y8 and y_scale come together", who);
-  if (!y8 && !y16 && !x_out) return reportf(SX_EINVAL, "%s: no output", who);
+  if (!y8 && !y16 && !x_out && total > 0) return reportf(SX_EINVAL, "%s: no output", who);
   if (x_out && !delta) return reportf(SX_EINVAL, "%s: x_out needs delta", who);
   if (y16 && !gamma) return reportf(SX_EINVAL, "%s: y16 needs gamma", who);
   if (gamma && (!(eps > 0.0f) || !std::isfinite(eps))) return reportf(SX_EINVAL, "%s: eps must be finite and > 0", who);
@@ -171,7 +171,7 @@ sx_status sx_silu_mul_f8(const sx_plan* plan, const int32_t* n_rows, int32_t max
   sx_status st = rows_of(who, plan, nullptr, n_rows, max_rows, false, stream, &a.r, &total);
   if (st != SX_OK) return st;
   if ((st = width_ok(who, "f", f, 1 << 24)) != SX_OK) return st;
-  if (!gate_up || !y8 || !y_scale) return reportf(SX_EINVAL, "%s: NULL argument", who);
+  if ((!gate_up || !y8 || !y_scale) && total > 0) return reportf(SX_EINVAL, "%s: NULL argument", who);
   const Arg in[] = {{gate_up, total * 4 * f, "gate_up"}, n_rows_arg(plan, n_rows)};
   const Arg out[] = {{y8, total * f, "y8"}, {y_scale, total * sx::f8_ld(f), "y_scale"}};
   const Arg wide[] = {in[0]};
@@ -197,14 +197,14 @@ sx_status sx_gemm_f8(const sx_plan* plan, const int32_t* rows, const int32_t* n_
   int64_t total;
   sx_status st = rows_of(who, plan, rows, n_rows, max_rows, x_by_token || y_by_token, stream, &a.r, &total);
   if (st != SX_OK) return st;
-  if (!x8 || !x_scale || !w8 || !w_scale || !part_n || !y_parts) return reportf(SX_EINVAL, "%s: NULL argument", who);
+  if (((!x8 || !x_scale) && total > 0) || !w8 || !w_scale || !part_n || !y_parts) return reportf(SX_EINVAL, "%s: NULL argument", who);
   if (n_parts < 1 || n_parts > sx::kF8MaxParts) return reportf(SX_EINVAL, "%s: n_parts %d outside 1..%d", who, n_parts, sx::kF8MaxParts);
   if (residual && n_parts != 1) return reportf(SX_EINVAL, "%s: a residual needs one part", who);
   if ((st = width_ok(who, "k", k, sx::kF8MaxK)) != SX_OK) return st;
   int64_t n = 0;
   Arg out[sx::kF8MaxParts] = {{nullptr, 0, "y"}, {nullptr, 0, "y part 1"}, {nullptr, 0, "y part 2"}, {nullptr, 0, "y part 3"}};
   for (int i = 0; i < n_parts; ++i) {
-    if (!y_parts[i]) return reportf(SX_EINVAL, "%s: output part %d is NULL", who, i);
+    if (!y_parts[i] && total > 0) return reportf(SX_EINVAL, "%s: output part %d is NULL", who, i);
     if ((st = width_ok(who, "a part's width", part_n[i], 1 << 24)) != SX_OK) return st;
     a.y[i] = (uint16_t*)y_parts[i];
     a.pn[i] = (int)n;
@@ -257,7 +257,7 @@ sx_status sx_moe_route(const sx_plan* plan, const int32_t* n_rows, int32_t max_r
   if (st != SX_OK) return st;
   if (logits_dtype != SX_F32 && logits_dtype != SX_BF16) return reportf(SX_EUNSUPPORTED, "%s: logits_dtype %d", who, logits_dtype);
   if ((st = sx_moe_route_workspace(n_experts, top_k, a.r.n_req, max_rows, &need)) != SX_OK) return st;
-  if (!logits || !ids || !weights || !offsets || !order || !workspace) return reportf(SX_EINVAL, "%s: NULL argument", who);
+  if (((!logits || !ids || !weights || !order) && total > 0) || !offsets || !workspace) return reportf(SX_EINVAL, "%s: NULL argument", who);
   if (workspace_bytes < need)
     return reportf(SX_ESHAPE, "%s needs %lld bytes of workspace, got %lld", who, (long long)need, (long long)workspace_bytes);
   if (total * top_k > INT32_MAX) return reportf(SX_EUNSUPPORTED, "%s: %lld rows x %d experts exceed 2^31", who, (long long)total, top_k);
@@ -342,7 +342,7 @@ sx_status sx_moe_combine(const sx_plan* plan, const int32_t* rows, const int32_t
   if (st != SX_OK) return st;
   if (top_k < 1 || top_k > sx::kMoeMaxTop) return reportf(SX_EUNSUPPORTED, "%s: top_k %d outside 1..%d", who, top_k, sx::kMoeMaxTop);
   if (h <= 0 || h % 8 != 0 || h > (1 << 24)) return reportf(SX_EUNSUPPORTED, "%s needs h a positive multiple of 8 up to 2^24 (%d)", who, h);
-  if (!y || !weights || !out) return reportf(SX_EINVAL, "%s: NULL argument", who);
+  if ((!y || !weights || !out) && total > 0) return reportf(SX_EINVAL, "%s: NULL argument", who);
   const Arg in[] = {{y, total * top_k * 2 * h, "y"}, {residual, total * 2 * h, "residual"}, {weights, 4 * total * top_k, "weights"},
                     rows_arg(plan, rows), n_rows_arg(plan, n_rows)};
   const Arg to[] = {{out, total * 2 * h, "out"}};

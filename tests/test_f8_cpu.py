@@ -175,6 +175,24 @@ def test_nothing_to_do_is_fine():
     assert sx.lib().sx_f8_pack_weight(None, 0, 128, None, None, None) == ok
 
 
+def test_arrays_of_no_rows_may_be_null():
+    # as empty tensors are
+    ok = sx.SX_OK
+    assert norm(m=0, x=None, delta=None, xo=None, y16=None, y8=None, ys=None) == ok
+    assert gemm(m=0, x=None, xs=None, y=(None, None)) == ok and gemm(m=0, x=None, xs=None, parts=1, y=(None,), res=None) == ok
+    assert silu(m=0, gu=None, y8=None, ys=None) == ok and combine(m=0, y=None, wt=None, res=None, out=None) == ok
+    assert experts(places=0, xr=0, off=None, order=None, x=None, xs=None, y=None) == ok
+    # what has no rows of its own may not
+    err(gemm(m=0, w=None), V, "NULL")
+    err(gemm(m=0, ws=None), V, "NULL")
+    err(gemm(m=0, y=None), V, "NULL")
+    err(route(m=0, off=None), V, "NULL")
+    err(route(m=0, ws=None), V, "NULL")
+    # with rows, nor may they
+    err(norm(m=1, x=None), V, "x is NULL")
+    err(gemm(m=1, y=(at(5), None)), V, "part 1 is NULL")
+
+
 @pytest.mark.parametrize("args,want,text", [
     ((at(0), 100, 128, at(1), at(2), None), U, "multiple"), ((at(0), 128, 64, at(1), at(2), None), U, "multiple"),
     ((None, 128, 128, at(1), at(2), None), V, "NULL"), ((at(0), 128, 128, at(0), at(2), None), V, "overlaps"),

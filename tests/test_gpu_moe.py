@@ -370,3 +370,31 @@ def test_a_mixture_captured_and_replayed():
                 near16(b["y"][i * top + j][None], t, R.product_bound(f, m), "down")
         t = b["y"].view(rows, top, h)[:n].double() * b["w"][:n, :, None].double()
         near16(b["out"][:n], want + t.sum(1), (top + 1) * R.E * (mag + t.abs().sum(1)), "mixture")
+
+
+def test_batches_of_no_rows():
+    # every call of both chains; a routing of no rows has offsets of 0
+    g = gen(41)
+    h, f, e, top = 256, 384, 6, 2
+    wg, wd = [t.cuda() for t in expert_weights(g, e, 2 * f, h)], [t.cuda() for t in expert_weights(g, e, h, f)]
+    gamma = torch.ones(h, dtype=BF16, device="cuda")
+    z = lambda *s, d=BF16: torch.zeros(*s, dtype=d, device="cuda")  # noqa: E731
+    x, a8, as_ = z(0, h), z(0, h, d=F8), z(0, R.ld(h), d=torch.uint8)
+    off = torch.full((e + 1,), -7, dtype=torch.int32, device="cuda")
+    ws = z(sx.moe_route_workspace(e, top, 0), d=torch.uint8)
+    ids, w, order = z(0, top, d=torch.int32), z(0, top, d=torch.float32), z(0, d=torch.int32)
+    sx.add_rmsnorm_f8(x, a8, as_, gamma=gamma, delta=z(0, h), x_out=x, y16=z(0, h))
+    sx.add_rmsnorm_f8(x, a8, as_)
+    sx.gemm_f8(a8, as_, wg[0][0], wg[1][0], [z(0, f), z(0, f)])
+    sx.gemm_f8(z(0, f, d=F8), z(0, R.ld(f), d=torch.uint8), wd[0][0], wd[1][0], x, residual=x)
+    for dtype in (torch.float32, BF16):
+        for n_rows in (None, i32([3])):     # (whatever a padded batch's count says)
+            off.fill_(-7)
+            sx.moe_route(z(0, e, d=dtype), ids, w, off, order, ws, n_rows=n_rows)
+            assert not off.any()
+    gu, f8, fs = z(0, 2 * f), z(0, f, d=F8), z(0, R.ld(f), d=torch.uint8)
+    sx.gemm_experts_f8(a8, as_, *wg, off, order, gu, gather=top)
+    sx.silu_mul_f8(gu, f8, fs, n_rows=off[-1:])
+    sx.gemm_experts_f8(f8, fs, *wd, off, order, z(0, h), scatter=True)
+    sx.moe_combine(z(0, h), w, x, residual=x)
+    torch.cuda.synchronize()
