@@ -787,14 +787,11 @@ int64_t count_tiles(const F8GemmK& a, int bm) {
   return a.n_places / bm + (int64_t)(a.n_experts < a.n_places ? a.n_experts : a.n_places);
 }
 
-template <int FI, int RJ, int D>
+template <int FI, int RJ, int D, bool EXPERTS>
 hipError_t launch_stream(F8GemmK& a, hipStream_t s) {
   a.m_tiles = (int)(((int64_t)a.r.max_rows + 16 * RJ - 1) / (16 * RJ));
   const int64_t blocks = count_tiles(a, 16 * RJ) * (a.N / (16 * FI));
-  if (a.offsets)
-    hipLaunchKernelGGL((f8_stream_kernel<FI, RJ, D, true>), dim3((unsigned)blocks), dim3(64), 0, s, a);
-  else
-    hipLaunchKernelGGL((f8_stream_kernel<FI, RJ, D, false>), dim3((unsigned)blocks), dim3(64), 0, s, a);
+  hipLaunchKernelGGL((f8_stream_kernel<FI, RJ, D, EXPERTS>), dim3((unsigned)blocks), dim3(64), 0, s, a);
   return hipGetLastError();
 }
 
@@ -836,10 +833,12 @@ hipError_t launch_pair(F8GemmK& a, int n_cu, hipStream_t s) {
   return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, kRun, s, f8_pair_kernel<BN, BM, WN, WM, NST, false>,
                                            f8_pair_kernel<BN, BM, WN, WM, NST, true>);
 }
-template <int BN, int BM, int WN, int WM, int NST>
+// GROUPED: for rows grouped by expert too.
+template <int BN, int BM, int WN, int WM, int NST, bool GROUPED>
 hipError_t launch_narrow(F8GemmK& a, int n_cu, hipStream_t s) {
+  if (!GROUPED && a.offsets) return hipErrorInvalidConfiguration;
   return launch_tiled<BN, BM, WN, WM, NST>(a, n_cu, 1, s, f8_narrow_kernel<BN, BM, WN, WM, NST, false>,
-                                           f8_narrow_kernel<BN, BM, WN, WM, NST, true>);
+                                           f8_narrow_kernel<BN, BM, WN, WM, NST, GROUPED>);
 }
 
 // What a launch of a shape takes, fitted to 105 products of 1 to 6712 rows by seven weights of 768 to 14336 x 1024 to 28672,
@@ -901,16 +900,16 @@ int best_shape(const F8GemmK& a, int n_cu) {
 hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
   switch (best_shape(a, n_cu)) {
     case kStream:
-      if (a.offsets) return launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4>(a, s);
+      if (a.offsets) return launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4, true>(a, s);
       // Blocks ahead: 16 of them leave room for one wave a SIMD, which then has more on its way (1 row x 4096 x 14336 17.0 us,
       // 18.3 with 12, 20.3 with 8); where there are more waves, or few blocks, 12 (1 x 28672 x 4096 27.7, 29.6 with 16).
-      if (a.K >= 16 * kF8Group && count_tiles(a, 16) * (a.N / 16) <= 4 * (int64_t)n_cu) return launch_stream<1, 1, 16>(a, s);
-      return launch_stream<1, 1, 12>(a, s);
-    case k32x32: return launch_narrow<32, 32, 2, 2, 6>(a, n_cu, s);
-    case k64x32: return launch_narrow<64, 32, 2, 2, 6>(a, n_cu, s);
-    case k64x64: return launch_narrow<64, 64, 2, 2, 4>(a, n_cu, s);
-    case k128x64: return launch_narrow<128, 64, 4, 2, 3>(a, n_cu, s);
-    case k128x128: return launch_narrow<128, 128, 4, 2, 4>(a, n_cu, s);
+      if (a.K >= 16 * kF8Group && count_tiles(a, 16) * (a.N / 16) <= 4 * (int64_t)n_cu) return launch_stream<1, 1, 16, false>(a, s);
+      return launch_stream<1, 1, 12, false>(a, s);
+    case k32x32: return launch_narrow<32, 32, 2, 2, 6, false>(a, n_cu, s);
+    case k64x32: return launch_narrow<64, 32, 2, 2, 6, false>(a, n_cu, s);
+    case k64x64: return launch_narrow<64, 64, 2, 2, 4, false>(a, n_cu, s);
+    case k128x64: return launch_narrow<128, 64, 4, 2, 3, true>(a, n_cu, s);
+    case k128x128: return launch_narrow<128, 128, 4, 2, 4, true>(a, n_cu, s);
     case k128x128x2: return launch_pair<128, 128, 4, 2, 2>(a, n_cu, s);
     case k256x256: return launch_tile<256, 256, 2, 2, 2>(a, n_cu, s);
     default: return hipErrorInvalidConfiguration;   // (more workgroups than a launch has)

@@ -1,12 +1,14 @@
 """The 8-bit layer body without a GPU: refusals of the C entry points and of the binding, and the references' own checks."""
 import ctypes
 import math
+import re
 
 import pytest
 import torch
 
 import f8ref as R
 import paper_2606_01751_amd as sx
+from test_wait_states_cpu import built  # noqa: F401
 
 A = 1 << 30          # an address that no refused call reads
 S = 1 << 26          # arguments lie this far apart
@@ -229,6 +231,22 @@ def test_binding_refuses_what_is_not_on_the_gpu():
               lambda: sx.gemm_experts_f8(c, s, c[None], s, s, None, x)):
         with pytest.raises(ValueError, match="not on the current GPU"):
             f()
+
+
+def test_product_kernels_are_those_that_a_call_can_take(built):  # noqa: F811
+    # listed rows: every shape; grouped ones: streamed two by two, or tiles from 128 x 64 on
+    rows, grouped = 0, 1
+    want = {("stream", (1, 1, 12, rows)), ("stream", (1, 1, 16, rows)), ("stream", (2, 2, 4, grouped)),
+            ("narrow", (32, 32, 2, 2, 6, rows)), ("narrow", (64, 32, 2, 2, 6, rows)), ("narrow", (64, 64, 2, 2, 4, rows))}
+    for g in (rows, grouped):
+        want |= {("narrow", (128, 64, 4, 2, 3, g)), ("narrow", (128, 128, 4, 2, 4, g)), ("pair", (128, 128, 4, 2, 2, g)),
+                 ("tile", (256, 256, 2, 2, 2, g))}
+    got = set()
+    for name, _ in built:
+        m = re.search(r"f8_(\w+)_kernelI((?:L[ib]\d+E)+)E", name)
+        if m and m[1] in ("stream", "narrow", "pair", "tile"):
+            got.add((m[1], tuple(int(v) for v in re.findall(r"L[ib](\d+)E", m[2]))))
+    assert got == want
 
 
 # ---- the references ----
