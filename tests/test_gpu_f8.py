@@ -352,6 +352,28 @@ def test_gemm_f8_large_launches(rows, n, k):
     near16(two[:3].cpu(), want + r, R.product_bound(k, mag + r.abs()), "three rows, residual")
 
 
+@pytest.mark.parametrize("rows,n,k", [(1, 19200, 4224), (4, 17408, 4096), (3, 20480, 3328), (1, 16512, 5248), (2, 18048, 1664)])
+def test_gemm_f8_few_rows_of_many_features(rows, n, k):
+    # more than 1024 waves that each read 12 blocks ahead, 13 to 41 blocks of k: every place is refilled, most of them twice.
+    # The bits are those of the same rows among 60 others, whose tiles go through LDS
+    g = gen(n + k)
+    x, xs = codes(g, rows + 60, k)
+    w, ws = codes(g, 0, k, n)
+    res = torch.randn(rows + 60, n, generator=g).to(BF16).cuda()
+    parts = [n - 768, 128, 640]
+    ys = [torch.full((rows, p), 7.0, dtype=BF16, device="cuda") for p in parts]
+    sx.gemm_f8(x[:rows], xs[:rows], w, ws, ys)
+    y, z, all_y, all_z = torch.cat(ys, 1), res[:rows].clone(), torch.empty_like(res), torch.empty_like(res)
+    sx.gemm_f8(x[:rows], xs[:rows], w, ws, z, residual=z)
+    sx.gemm_f8(x, xs, w, ws, all_y)
+    sx.gemm_f8(x, xs, w, ws, all_z, residual=res)
+    assert torch.equal(y, all_y[:rows]) and torch.equal(z, all_z[:rows])
+    want, mag = R.product(x[:rows].cpu(), xs[:rows].cpu(), w.cpu(), ws.cpu())
+    near16(y, want, R.product_bound(k, mag), "streamed")
+    r = res[:rows].cpu().double()
+    near16(z, want + r, R.product_bound(k, mag + r.abs()), "streamed, residual")
+
+
 @pytest.mark.parametrize("rows,k", [(5, 65536), (300, 65536), (700, 40064)])
 def test_gemm_f8_of_long_rows(rows, k):
     g = gen(rows + k)
