@@ -111,8 +111,10 @@ sx_status sx_moe_route(const sx_plan* plan, const int32_t* n_rows, int32_t max_r
 
 /* Products grouped by expert: for every expert e and every place p of offsets[e] .. offsets[e + 1] - 1,
  *   y[y row] = x[x row] . w[e]^T
- * with w8 [n_experts][n][k], w_scale [n_experts][n / 128][ld], x8, x_scale [x_rows][k], y [n_places][n] bfloat16.
- *   gather   0: the x row is p; else order[p] / gather (the row that place p stands for, gather = top_k)
+ * with w8 [n_experts][n][k], w_scale [n_experts][n / 128][ld], x8, x_scale [x_rows][k], y [n_places][n] bfloat16, rounded
+ * once as in sx_gemm_f8: of the down projection that is one rounding of each expert's result before their weighted sum.
+ *   gather   0: the x row is p (a place from x_rows on is out of range); else order[p] / gather (the row that place p
+ *            stands for, gather = top_k)
  *   scatter  0: the y row is p; else order[p] (the layout that sx_moe_combine reads)
  * order may be NULL when gather and scatter are 0.  offsets [n_experts + 1] and order [n_places] are DEVICE int32, as
  * sx_moe_route writes them; n_places (host) bounds offsets[n_experts].  n_experts <= 65536. */

@@ -333,12 +333,13 @@ __global__ __launch_bounds__(64, 1) void f8_stream_kernel(F8GemmK a) {
 //
 // Bound: by the matrix cores and LDS alike in the largest tiles, 256 x 256 by four waves of 128 x 128 with their 256 sums in
 // accumulation registers: of a block 2112 cycles of matrix instructions, 1344 of transfers and 1024 of reads.  6712 x
-// 28672 x 4096 in 621 us, 2.54 PFLOP/s; without storing results 552, of which the exchange through LDS is 2 us a tile and
-// the stores are 4.5.  By LDS and the length of the chain over k in the small ones: see there.
+// 28672 x 4096 in 617 to 644 us by the card's clock, 2.45 to 2.55 PFLOP/s; without storing results 552 where it took 621: a
+// tile's exchange through LDS is 2 us, its stores are 4.5.  By LDS and the length of the chain over k in the small ones: see
+// there.
 // ---------------------------------------------------------------------------------------------
 constexpr int kLdsBytes = 163840;   // LDS of a compute unit
 constexpr unsigned kXcds = 8;       // XCDs of the chip, which deals workgroups round-robin
-constexpr int kRowGroup = 8;        // row tiles per group of the tile order (6712 x 28672 x 4096: of 4, 8, 16 653, 657, 674 us)
+constexpr int kRowGroup = 8;        // row tiles per group of the tile order (6712 x 28672 x 4096: of 4, 8, 16 625, 640, 647 us)
 
 // s_waitcnt with vmcnt <= n (n < 64), expcnt and lgkmcnt left unconstrained (gfx9 encoding)
 #define SX_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | ((((n) >> 4) & 3) << 14) | (0x7 << 4) | (0xF << 8))
@@ -631,7 +632,7 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void f8_tile_kernel(F8GemmK a) {
 }
 
 // Tiles of which two workgroups share a compute unit and fill each other's waits: a block is read, the next one's transfers
-// go out, the block's matrix instructions run.  2048 x 4096 x 4096 43 us (1.6 PFLOP/s), 48 by 128 x 128 tiles read ahead, 60 by
+// go out, the block's matrix instructions run.  2048 x 4096 x 4096 43 us (1.6 PFLOP/s), 46 by 128 x 128 tiles read ahead, 59 by
 // 256 x 256.
 template <int BN, int BM, int WN, int WM, int NST, bool EXPERTS>
 __global__ __launch_bounds__(WN * WM * 64, 1) void f8_pair_kernel(F8GemmK a) {
@@ -797,8 +798,8 @@ hipError_t launch_stream(F8GemmK& a, hipStream_t s) {
 
 // Grid and LDS of a tiled launch, in runs of up to `most` tiles: as long as the workgroups of whole rounds then take no
 // more tiles each than in shorter ones.  A run fetches its next tile while it computes and stores the last: 6712 x 28672 x
-// 4096 in 256 x 256 tiles 632 us by runs of 4, 697 singly; 8192 tokens x 8 of 128 experts, 2048 -> 768 554 and 592, 768 -> 2048
-// 206 and 261; of 8 no faster than of 4.
+// 4096 in 256 x 256 tiles 635 us by runs of 4, 642 of 2, 660 singly; 8192 tokens x 8 of 128 experts, 768 -> 2048 202, 207 and
+// 231, 2048 -> 2 x 768, with 16 blocks a tile, 304 to 323 whatever the run; of 8 no faster than of 4.
 constexpr int kRun = 4;
 template <int BN, int BM, int WN, int WM, int NST, typename K>
 hipError_t launch_tiled(F8GemmK& a, int n_cu, int most, hipStream_t s, K plain, K experts) {
@@ -857,15 +858,17 @@ constexpr Shape kShape[kShapes] = {
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 4096;   // of a launch (and room for the grid's rounding)
 constexpr int kStreamExperts = 32;   // tile side of the streaming kernel for grouped rows (of listed ones: 16)
 
-// The shape of least time; for those 105 products within 4% of the fastest (0.1% in the mean).  Some of them in us, the shape
-// taken and its neighbours in the table: K = 4096, 1 row x 4096 features 7.9 (9.9), 1 x 6144 9.5 (10.8), 17 x 6144 10.2 (13.9,
-// 10.9), 64 x 6144 11.8 (13.9, 14.2), 200 x 4096 13.2 (16.3, 18.1), 394 x 4096 18.5 (19.7, 22.2), 1000 x 4096 25.2 (28.8, 37.2),
-// 2048 x 4096 43 (48, 60), 6712 x 28672 669 (881).
+// The shape of least time; for those 105 products within 4% of the fastest (0.1% in the mean).  Some of them in us, weights
+// from memory, the shape taken and its neighbours in the table: K = 4096, 1 row x 4096 features 8.0 (10.0), 1 x 6144 9.6 (10.1),
+// 17 x 6144 10.4 (13.9, 11.1), 64 x 6144 12.0 (14.0, 14.1), 200 x 4096 13.2 (16.5, 18.1), 394 x 4096 18.4 (19.9, 22.2), 1000 x 4096
+// 24.4 (28.7, 37.0), 2048 x 4096 42 (46, 59), 6712 x 28672 635 (845).  The costs hold no bound by the weights' bytes: of few rows
+// by many features they give less than memory takes (1 x 28672 x 4096, 117 MB: 16.8 us, where four shapes take 27.4 to 28.5), but
+// memory makes the shapes alike there.
 // Grouped rows: few for each expert, by the streaming kernel, since the weights' way from memory is the bound (64 tokens x 8
-// of 128 experts, 2048 -> 1536: 63 us, 71 of 128 x 64 tiles; 256 x 8, twice as wide: 185, 166); else by the same costs and as
-// many tiles as rows spread over the experts make, each expert's last one half full (2048 -> 2 x 1536: 512 x 8 of 128 193 us of
-// 128 x 64, 213 of 128 x 128; 2048 x 2 of 8 42 of 128 x 128, 48 of 128 x 64, 60 of 256 x 256; 8192 x 8 of 128 574 of 256 x 256, 688 of
-// 128 x 128; of 26 such products within 7% of the fastest but for five, which are 9 to 20% off).
+// of 128 experts, 2048 -> 2 x 768: 68 us, 71 of 128 x 64 tiles; 256 x 8: 98, 87); else by the same costs and as many tiles as
+// rows spread over the experts make, each expert's last one half full (2048 -> 2 x 768: 512 x 8 of 128 98 us of 128 x 64, 116 of
+// 128 x 128; 2048 x 2 of 8 24 of 128 x 128 by twos, 30 of 128 x 64, 35 of 256 x 256; 8192 x 8 of 128 304 to 320 of 256 x 256, 356
+// of 128 x 128; of 26 products within 7% of the fastest but for five, which are 9 to 20% off).
 int best_shape(const F8GemmK& a, int n_cu) {
   const bool ex = a.offsets;
   if (ex && a.n_places <= 12 * (int64_t)a.n_experts && count_tiles(a, kStreamExperts) * (a.N / kStreamExperts) * 64 < kMaxThreads)
@@ -901,8 +904,8 @@ hipError_t launch_gemm_f8(F8GemmK& a, int n_cu, hipStream_t s) {
   switch (best_shape(a, n_cu)) {
     case kStream:
       if (a.offsets) return launch_stream<kStreamExperts / 16, kStreamExperts / 16, 4, true>(a, s);
-      // Blocks ahead: 16 of them leave room for one wave a SIMD, which then has more on its way (1 row x 4096 x 14336 17.0 us,
-      // 18.3 with 12, 20.3 with 8); where there are more waves, or few blocks, 12 (1 x 28672 x 4096 27.7, 29.6 with 16).
+      // Blocks ahead: 16 of them leave room for one wave a SIMD, which then has more on its way (1 row x 4096 x 14336 17.1 us,
+      // 18.3 with 12, 20.3 with 8); where there are more waves, or few blocks, 12 (1 x 19200 x 4096 21.4, 24.8 with 16).
       if (a.K >= 16 * kF8Group && count_tiles(a, 16) * (a.N / 16) <= 4 * (int64_t)n_cu) return launch_stream<1, 1, 16, false>(a, s);
       return launch_stream<1, 1, 12, false>(a, s);
     case k32x32: return launch_narrow<32, 32, 2, 2, 6, false>(a, n_cu, s);
